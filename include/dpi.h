@@ -78,7 +78,9 @@ typedef enum {
   DPI_ERR_HIP = 7                  /* HIP runtime error; text in dpi_last_error() */
 } dpi_status;
 
-typedef enum { DPI_F32 = 0, DPI_F16 = 1 } dpi_dtype;
+typedef enum { DPI_F32 = 0, DPI_F16 = 1,
+               DPI_BF16 = 2                 /* dpi_embed_*, dpi_glr_* and dpi_adamw_* only */
+} dpi_dtype;
 typedef enum { DPI_POOL_SUM = 0, DPI_POOL_MEAN = 1 } dpi_pooling;
 typedef enum { DPI_X_F32 = 0, DPI_X_I64 = 1, DPI_X_I32 = 2 } dpi_x_dtype;   /* host feature matrix */
 
@@ -424,6 +426,171 @@ dpi_status dpi_plan_export_waves(dpi_plan_t plan, int64_t* wave_bag, int64_t* wa
 
 /* Free the host object (not the workspace).  NULL is ignored. */
 void dpi_plan_destroy(dpi_plan_t plan);
+
+/*
+ * Behaviour sequences: a user's history is a sequence of item ids in time
+ * order.  Histories are packed: the tokens of all sequences lie one after the
+ * other, offsets [num_seqs + 1] (device int32, offsets[0] = 0, non-decreasing,
+ * offsets[num_seqs] = number of tokens) delimit them, a sequence may be empty.
+ * Below, a row stride counts elements from one token's row to the next, so a
+ * block may be part of a wider one; rows whose base and stride are a multiple
+ * of 16 bytes are read fastest, any element-aligned ones are accepted.
+ *   device_status: NULL, or device int32 into which the call ORs
+ *   DPI_DEVSTAT_* bits (asynchronously); the caller clears it.
+ * Sums, scans and states are fp32; each output is rounded once (to nearest
+ * even).  Equal inputs give equal bits.
+ */
+
+/*
+ * Rows of one table for a list of tokens, scaled:
+ *   out[i][c] = scale * table[ids[i]][c].
+ * A token whose id is padding_id (negative: no padding) gets a row of zeros, so
+ * does an id outside [0, num_rows), which also sets DPI_DEVSTAT_BAD_ID.
+ *   table: device [num_rows][dim] of table_dtype;  ids: device int32 [num_tokens];
+ *   out:   device [num_tokens] rows of out_dtype, out_stride >= dim.
+ * Errors: INVALID_ARG (NULL, negative sizes, dim < 1, a stride below dim, bad
+ * dtype), UNSUPPORTED (dim > DPI_MAX_DIM, num_rows or num_tokens >= 2^31),
+ * MISALIGNED (a pointer not aligned to its elements), HIP.
+ */
+dpi_status dpi_embed_forward(const void* table, int32_t table_dtype, int64_t num_rows, int32_t dim,
+                             const int32_t* ids, int64_t num_tokens, float scale, int32_t padding_id, void* out,
+                             int32_t out_dtype, int64_t out_stride, int32_t* device_status, void* stream);
+
+/* Bytes of device workspace of dpi_embed_backward (0 on invalid arguments). */
+size_t dpi_embed_workspace_bytes(int64_t num_rows, int32_t dim, int64_t num_tokens);
+
+/*
+ * The table's gradient of dpi_embed_forward:
+ *   grad[v][c] = scale * sum over tokens i with ids[i] = v of dout[i][c],
+ * every element of grad written (rows without tokens, and the padding row, with
+ * zeros).  Tokens are sorted by id and each row's are added in a fixed order.
+ *   dout: device [num_tokens] rows of dout_dtype;
+ *   grad: device [num_rows][dim] of grad_dtype;
+ *   workspace: device, 16-byte aligned, one call in flight per workspace.
+ * Errors: as dpi_embed_forward; WORKSPACE_TOO_SMALL.
+ */
+dpi_status dpi_embed_backward(const void* dout, int32_t dout_dtype, int64_t dout_stride, const int32_t* ids,
+                              int64_t num_tokens, float scale, int32_t padding_id, void* grad, int32_t grad_dtype,
+                              int64_t num_rows, int32_t dim, void* workspace, size_t workspace_bytes,
+                              int32_t* device_status, void* stream);
+
+/*
+ * Gated linear recurrence over packed sequences: for token t of sequence s and
+ * every channel,
+ *   a_t = 1 / (1 + exp(-gate_t)),   h_t = a_t h_{t-1} + (1 - a_t) x_t,
+ * with h before the first token = h0[s] (0 without h0).  A gate of +infinity
+ * keeps the state.
+ */
+typedef struct {
+  int64_t num_tokens;
+  int64_t num_seqs;
+  int32_t dim;              /* channels */
+  int32_t dtype;            /* of x, gate, h and their gradients */
+  int64_t max_len;          /* a bound on the sequences' lengths, or 0: sets how the work is split, not the result */
+  const int32_t* offsets;   /* device [num_seqs + 1] */
+  const void* x;            /* device, num_tokens rows */
+  const void* gate;
+  int64_t x_stride;
+  int64_t gate_stride;
+  const float* h0;          /* device [num_seqs][dim], or NULL */
+} dpi_glr_desc;
+
+/* Bytes of the states that a forward pass saves for the backward pass of the
+ * same sizes (0 on invalid arguments). */
+size_t dpi_glr_entry_bytes(const dpi_glr_desc* desc);
+
+/* Bytes of device workspace of either pass; 0 on invalid arguments, at least 16 otherwise. */
+size_t dpi_glr_workspace_bytes(const dpi_glr_desc* desc);
+
+/*
+ * Forward pass.
+ *   h:      device, num_tokens rows of desc->dtype (h_stride >= dim);
+ *   h_last: NULL, or device fp32 [num_seqs][dim]: the state after each
+ *           sequence's last token (its h0, or 0, for an empty one);
+ *   entry:  NULL, or dpi_glr_entry_bytes of device memory for the backward pass;
+ *   workspace: device, 16-byte aligned, one call in flight per workspace.
+ * h must not overlap an input.  Malformed offsets set DPI_DEVSTAT_BAD_OFFSETS
+ * and leave the outputs unspecified.
+ * Errors: INVALID_ARG, UNSUPPORTED (dim > DPI_MAX_DIM, num_tokens or num_seqs
+ * >= 2^31), MISALIGNED, WORKSPACE_TOO_SMALL, HIP.
+ */
+dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, float* h_last, void* entry,
+                           void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream);
+
+/*
+ * Backward pass: from dh (gradient of h; NULL: zeros) and dh_last (gradient of
+ * h_last, fp32 [num_seqs][dim]; NULL: zeros),
+ *   e_t = dh_t + a_{t+1} e_{t+1} (dh_t + dh_last[s] at the last token),
+ *   dx_t = (1 - a_t) e_t,   dgate_t = a_t (1 - a_t) (h_{t-1} - x_t) e_t,
+ *   dh0[s] = a_0 e_0 (dh_last[s] for an empty sequence).
+ * States are computed again in fp32 from x, gate and `entry`, which is what the
+ * forward pass over the same desc wrote.
+ *   dx, dgate: device rows of desc->dtype;  dh0: NULL, or device fp32 [num_seqs][dim].
+ */
+dpi_status dpi_glr_backward(const dpi_glr_desc* desc, const void* entry, const void* dh, int64_t dh_stride,
+                            const float* dh_last, void* dx, int64_t dx_stride, void* dgate, int64_t dgate_stride,
+                            float* dh0, void* workspace, size_t workspace_bytes, int32_t* device_status,
+                            void* stream);
+
+/*
+ * One token for each of `batch` sequences whose states lie in a store:
+ *   state[slot] = a state[slot] + (1 - a) x[b],   h[b] = state[slot],
+ * slot = slots[b] (NULL: b).  Slots must be distinct (of rows that name one
+ * slot, which update stays is unspecified).  A slot outside [0, num_slots)
+ * gives a row of zeros, changes no state and sets DPI_DEVSTAT_BAD_ID.
+ *   state: device fp32 [num_slots][dim];  x, gate, h: device rows of dtype.
+ */
+dpi_status dpi_glr_step(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, int32_t dtype,
+                        int64_t batch, int32_t dim, float* state, int64_t num_slots, const int32_t* slots, void* h,
+                        int64_t h_stride, int32_t* device_status, void* stream);
+
+/*
+ * AdamW over many tensors in one launch (256 tensors a launch):
+ *   g = grad_scale * grad
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32.  With a master copy, p is the master, and param receives it rounded.
+ * States of 32 bits are fp32; states of 8 bits hold e4m3 codes and, for every
+ * DPI_ADAMW_BLOCK elements of a tensor, an fp32 scale (code * scale is the
+ * value): codes are rounded at random with the value as their mean, from a hash
+ * of (seed, step, tensor, element), and a nonzero v keeps a nonzero code.
+ */
+#define DPI_ADAMW_BLOCK 256
+typedef struct {
+  void* param;           /* device, of param_dtype */
+  float* master;         /* device, or NULL */
+  void* m;               /* device fp32, or uint8 with states of 8 bits */
+  void* v;
+  float* m_scale;        /* states of 8 bits: device [ceil(count / DPI_ADAMW_BLOCK)], else NULL */
+  float* v_scale;
+  int64_t count;         /* elements, contiguous */
+  int32_t param_dtype;
+  int32_t grad_dtype;
+} dpi_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  double grad_scale;     /* the gradients are multiplied by it (1 / loss scale, clipping) */
+  int64_t step;          /* t >= 1 */
+  uint32_t seed;
+} dpi_adamw_hyper;
+
+typedef struct dpi_adamw_s* dpi_adamw_t;
+
+/* Bytes of device workspace for these tensors (0 on invalid arguments). */
+size_t dpi_adamw_workspace_bytes(const dpi_adamw_tensor* tensors, int32_t num_tensors, int32_t state_bits);
+
+/* Check the tensors and copy their description into `workspace` (device,
+ * 16-byte aligned, outlives the handle); synchronous, not for graph capture.
+ * The handle borrows the tensors.  state_bits: 32 or 8. */
+dpi_status dpi_adamw_create(const dpi_adamw_tensor* tensors, int32_t num_tensors, int32_t state_bits,
+                            void* workspace, size_t workspace_bytes, dpi_adamw_t* out);
+
+/* One step, in place.  grads: host [num_tensors] of device pointers (NULL: that
+ * tensor is left as it is).  Errors: INVALID_ARG (lr, weight_decay, eps < 0,
+ * betas outside [0, 1), step < 1, not a number), MISALIGNED, HIP. */
+dpi_status dpi_adamw_step(dpi_adamw_t adamw, const void* const* grads, const dpi_adamw_hyper* hyper, void* stream);
+void dpi_adamw_destroy(dpi_adamw_t adamw);
 
 const char* dpi_status_str(dpi_status s);
 const char* dpi_last_error(void);   /* thread-local detail of the last error */

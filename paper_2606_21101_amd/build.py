@@ -9,7 +9,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdpi.so")
 SOURCES = ["api.cpp", "plan.hip", "lookup.hip", "small.hip", "fm.hip", "stage.hip", "interact.hip", "sched.cpp",
-           "noalloc.hip"]
+           "noalloc.hip", "embed.hip", "recur.hip", "adamw.hip", "seq_api.cpp"]
 ARCH = os.environ.get("DPI_OFFLOAD_ARCH", "gfx950")
 
 HIPCC_FLAGS = [

@@ -1,0 +1,210 @@
+// AdamW over many tensors in one launch, for gfx950 (MI355X).
+//
+//   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
+//   p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+//
+// A workgroup takes kAdamChunk elements of one tensor (its row of the chunk
+// table says which), a wave 256 elements at a time, a lane 4 neighbours.  The
+// bound is HBM: every array is read and written once.
+//
+// 8-bit states: 256 elements, one wave's, share a scale max|x| / 448 and hold
+// e4m3 codes (4 bits of exponent, 3 of mantissa).  Codes are rounded up or
+// down at random so that their mean is the value: a second moment moves by
+// 1 - beta2 = 0.1 % a step where neighbouring codes are 6 to 12 % apart, so
+// rounded to nearest it would never move.  A nonzero second moment keeps a
+// nonzero code: a zero one under a nonzero first moment would divide by eps.
+// The random bits are a hash of (seed, step, tensor, element): equal calls
+// give equal bits.
+#include "elem.h"
+#include "seq_internal.h"
+
+namespace dpi {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+// A 32-bit mixing: xor-shifts and products with odd constants (the fractions of sqrt 2 and sqrt 3).
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x6A09E667u;
+  x ^= x >> 15;
+  x *= 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+
+template <typename T>
+__device__ __forceinline__ void get4(const void* p, int64_t i, int have, bool wide, float* v) {
+  const T* q = static_cast<const T*>(p) + i;
+  const Elems<T, 4> e = wide ? load_elems<true, T, 4>(q, have) : load_elems<false, T, 4>(q, have);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = e[j];
+}
+
+__device__ __forceinline__ void get4(int32_t dtype, const void* p, int64_t i, int have, bool wide, float* v) {
+  if (dtype == DPI_F32)
+    get4<float>(p, i, have, wide, v);
+  else if (dtype == DPI_F16)
+    get4<f16_t>(p, i, have, wide, v);
+  else
+    get4<bf16_t>(p, i, have, wide, v);
+}
+
+template <typename T>
+__device__ __forceinline__ void put4(void* p, int64_t i, int have, bool wide, const float* v) {
+  T* q = static_cast<T*>(p) + i;
+  if (wide)
+    store_elems<true, T, 4>(q, v, have);
+  else
+    store_elems<false, T, 4>(q, v, have);
+}
+
+__device__ __forceinline__ void put4(int32_t dtype, void* p, int64_t i, int have, bool wide, const float* v) {
+  if (dtype == DPI_F32)
+    put4<float>(p, i, have, wide, v);
+  else if (dtype == DPI_F16)
+    put4<f16_t>(p, i, have, wide, v);
+  else
+    put4<bf16_t>(p, i, have, wide, v);
+}
+
+__device__ __forceinline__ void get4_codes(const void* p, int64_t i, int have, bool wide, float scale, float* v) {
+  const uint8_t* q = static_cast<const uint8_t*>(p) + i;
+  uint32_t w = 0;
+  if (wide) {
+    w = *reinterpret_cast<const uint32_t*>(q);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w |= (uint32_t)q[min(j, have - 1)] << (8 * j);
+  }
+  v[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale;
+  v[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale;
+  v[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale;
+  v[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * scale;
+}
+
+// |x| / scale, at most 448, to an e4m3 code: rnd (20 bits) is added below the
+// last kept bit of a normal code, and below the unit of a subnormal one.
+__device__ __forceinline__ uint32_t round8(float y, uint32_t rnd) {
+  const uint32_t normal = ((__float_as_uint(y) + rnd) >> 20) - (120u << 3);
+  const uint32_t small = (uint32_t)floorf(y * 512.f + (float)rnd * 0x1p-20f);
+  return y >= 0x1p-6f ? normal : small;
+}
+
+// A wave's 256 values (those past the tensor's end are 0) as codes and their scale.
+template <bool KEEP_SMALL>
+__device__ __forceinline__ void put4_codes(void* p, float* scale, int64_t i, int have, bool wide, const float* v,
+                                           const uint32_t* rnd) {
+  // largest magnitude by its bits: a NaN is larger than any number, so it spreads over the block and is seen
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+  const float amax = __uint_as_float(top);
+  const bool none = amax <= 0x1p-100f;   // 448 / amax would leave the range: held as zeros
+  const float inv = none ? 0.f : 448.f / amax;
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float y = fminf(fabsf(v[j]) * inv, 448.f);
+    uint32_t c = round8(y, rnd[j]);
+    if (KEEP_SMALL && y > 0.f) c = max(c, 1u);
+    c |= v[j] < 0.f ? 0x80u : 0u;
+    w |= (c & 0xffu) << (8 * j);
+  }
+  uint8_t* q = static_cast<uint8_t*>(p) + i;
+  if (have > 0) {
+    if (wide) {
+      *reinterpret_cast<uint32_t*>(q) = w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < have) q[j] = (uint8_t)(w >> (8 * j));
+    }
+  }
+  if ((threadIdx.x & 63) == 0) *scale = none ? 0.f : amax / 448.f;
+}
+
+__device__ __forceinline__ bool aligned_to(const void* p, int bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0;
+}
+
+__device__ __forceinline__ int size_of(int32_t dtype) { return dtype == DPI_F32 ? 4 : 2; }
+
+template <bool BITS8>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
+#pragma clang fp contract(off)
+  const AdamChunk c = a.chunks[a.first_chunk + blockIdx.x];
+  const void* grad = a.grads[c.tensor - a.first_tensor];
+  if (!grad) return;
+  const AdamTensor t = a.tensors[c.tensor];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t key = mix(a.seed + (uint32_t)c.tensor * 0xC2B2AE35u);
+  const bool whole = aligned_to(t.param, 4 * size_of(t.param_dtype)) && aligned_to(grad, 4 * size_of(t.grad_dtype)) &&
+                     aligned_to(t.master, 16) && aligned_to(t.m, BITS8 ? 4 : 16) && aligned_to(t.v, BITS8 ? 4 : 16);
+  for (int b = wave; b < kAdamChunk / kAdamBlock; b += kWaves) {
+    const int64_t block = (int64_t)c.chunk * (kAdamChunk / kAdamBlock) + b;
+    if (block * kAdamBlock >= t.count) return;   // the same for the whole wave
+    const int64_t i = block * kAdamBlock + lane * 4;
+    const int have = (int)min((int64_t)4, t.count - i);   // elements of this lane: 0 or less past the end
+    const bool wide = whole && have == 4;
+    float g[4], m[4], v[4], p[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = m[j] = v[j] = p[j] = 0.f;
+    if (have > 0) {
+      get4(t.grad_dtype, grad, i, have, wide, g);
+      if (t.master)
+        get4<float>(t.master, i, have, wide, p);
+      else
+        get4(t.param_dtype, t.param, i, have, wide, p);
+      if constexpr (BITS8) {
+        get4_codes(t.m, i, have, wide, t.m_scale[block], m);
+        get4_codes(t.v, i, have, wide, t.v_scale[block], v);
+      } else {
+        get4<float>(t.m, i, have, wide, m);
+        get4<float>(t.v, i, have, wide, v);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float gj = g[j] * a.grad_scale;
+      m[j] = m[j] * a.beta1 + gj * a.omb1;
+      v[j] = v[j] * a.beta2 + (gj * gj) * a.omb2;
+      p[j] = p[j] * a.decay - a.step_size * (m[j] / (sqrtf(v[j]) * a.root + a.eps));
+      if (j >= have) m[j] = v[j] = 0.f;   // a value past the end has no part in the scale
+    }
+    if (have > 0) {
+      if (t.master) put4<float>(t.master, i, have, wide, p);
+      put4(t.param_dtype, t.param, i, have, wide, p);
+    }
+    if constexpr (BITS8) {
+      uint32_t rm[4], rv[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t e = (uint64_t)(i + j);
+        const uint32_t r = mix((uint32_t)e * 0x9E3779B1u + (uint32_t)(e >> 32) + key);
+        rm[j] = (r & 0xffffu) << 4;
+        rv[j] = (r >> 16) << 4;
+      }
+      put4_codes<false>(t.m, t.m_scale + block, i, have, wide, m, rm);
+      put4_codes<true>(t.v, t.v_scale + block, i, have, wide, v, rv);
+    } else if (have > 0) {
+      put4<float>(t.m, i, have, wide, m);
+      put4<float>(t.v, i, have, wide, v);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamArgs& a, int64_t chunks, hipStream_t s) {
+  if (chunks <= 0) return hipSuccess;
+  if (a.bits8)
+    adamw_kernel<true><<<dim3((unsigned)chunks), kThreads, 0, s>>>(a);
+  else
+    adamw_kernel<false><<<dim3((unsigned)chunks), kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace dpi

@@ -1,0 +1,412 @@
+// C entry points of the behaviour-sequence operators and of AdamW: argument
+// checks, workspace layouts and launches (kernels in embed.hip, recur.hip,
+// adamw.hip).
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "elem.h"
+#include "seq_internal.h"
+
+using namespace dpi;
+
+__attribute__((visibility("hidden"))) dpi_status dpi_fail_status(dpi_status s, const char* fmt, ...);   // api.cpp
+__attribute__((visibility("hidden"))) dpi_status dpi_hip_status(hipError_t e, const char* what);        // api.cpp
+
+namespace {
+
+bool off_by(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
+
+dpi_status check_sizes(int64_t num_rows, int32_t dim, int64_t num_tokens) {
+  if (num_rows < 0 || num_tokens < 0) return dpi_fail_status(DPI_ERR_INVALID_ARG, "negative num_rows or num_tokens");
+  if (dim < 1) return dpi_fail_status(DPI_ERR_INVALID_ARG, "dim must be >= 1");
+  if (dim > DPI_MAX_DIM) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "dim %d > %d", dim, DPI_MAX_DIM);
+  if (num_rows > INT32_MAX || num_tokens > INT32_MAX)
+    return dpi_fail_status(DPI_ERR_UNSUPPORTED, "num_rows and num_tokens must be below 2^31");
+  return DPI_OK;
+}
+
+// One operand of token rows: `what` for the message.
+dpi_status check_rows(const void* p, int32_t dtype, int64_t stride, int32_t dim, int64_t rows, const char* what) {
+  if (stride < dim) return dpi_fail_status(DPI_ERR_INVALID_ARG, "%s: row stride below dim", what);
+  if (rows > 0 && stride > INT64_MAX / 8 / rows) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "%s: row stride too large", what);
+  if (rows > 0 && !p) return dpi_fail_status(DPI_ERR_INVALID_ARG, "%s is NULL", what);
+  if (off_by(p, elem_size(dtype))) return dpi_fail_status(DPI_ERR_MISALIGNED, "%s not element-aligned", what);
+  return DPI_OK;
+}
+
+dpi_status check_words(const void* p, bool needed, const char* what) {
+  if (needed && !p) return dpi_fail_status(DPI_ERR_INVALID_ARG, "%s is NULL", what);
+  if (off_by(p, 4)) return dpi_fail_status(DPI_ERR_MISALIGNED, "%s not 4-byte aligned", what);
+  return DPI_OK;
+}
+
+dpi_status check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (!ws) return dpi_fail_status(DPI_ERR_INVALID_ARG, "workspace is NULL");
+  if (off_by(ws, 16)) return dpi_fail_status(DPI_ERR_MISALIGNED, "workspace not 16-byte aligned");
+  if (bytes < need) return dpi_fail_status(DPI_ERR_WORKSPACE_TOO_SMALL, "workspace %zu bytes, need %zu", bytes, need);
+  return DPI_OK;
+}
+
+#define DPI_TRY(expr)                    \
+  do {                                   \
+    const dpi_status st_ = (expr);       \
+    if (st_ != DPI_OK) return st_;       \
+  } while (0)
+
+// ------------------------------------------------------------------ recurrence
+dpi_status check_glr(const dpi_glr_desc* d) {
+  if (!d) return dpi_fail_status(DPI_ERR_INVALID_ARG, "desc is NULL");
+  if (d->num_tokens < 0 || d->num_seqs < 0 || d->max_len < 0)
+    return dpi_fail_status(DPI_ERR_INVALID_ARG, "negative num_tokens, num_seqs or max_len");
+  if (d->dim < 1) return dpi_fail_status(DPI_ERR_INVALID_ARG, "dim must be >= 1");
+  if (!known_dtype(d->dtype)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "bad dtype");
+  if (d->dim > DPI_MAX_DIM) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "dim %d > %d", d->dim, DPI_MAX_DIM);
+  if (d->num_tokens > INT32_MAX || d->num_seqs >= INT32_MAX)
+    return dpi_fail_status(DPI_ERR_UNSUPPORTED, "num_tokens and num_seqs must be below 2^31");
+  if (d->num_tokens > 0 && d->num_seqs == 0)
+    return dpi_fail_status(DPI_ERR_INVALID_ARG, "num_seqs is 0 with num_tokens > 0");
+  return DPI_OK;
+}
+
+dpi_status check_glr_operands(const dpi_glr_desc* d) {
+  DPI_TRY(check_words(d->offsets, d->num_seqs > 0, "offsets"));
+  DPI_TRY(check_rows(d->x, d->dtype, d->x_stride, d->dim, d->num_tokens, "x"));
+  DPI_TRY(check_rows(d->gate, d->dtype, d->gate_stride, d->dim, d->num_tokens, "gate"));
+  return check_words(d->h0, false, "h0");
+}
+
+// Whether a thread's kGlrV channels are one aligned access in every row of these operands.
+struct Wide {
+  size_t access;
+  int elem;
+  bool ok;
+  Wide(int32_t dtype, int32_t dim) : access((size_t)kGlrV * elem_size(dtype)), elem(elem_size(dtype)), ok(dim % kGlrV == 0) {}
+  void add(const void* p, int64_t stride) { ok = ok && !off_by(p, access) && ((size_t)stride * elem) % access == 0; }
+};
+
+GlrArgs glr_args(const dpi_glr_desc* d, int32_t* status) {
+  GlrArgs a{};
+  a.offsets = d->offsets;
+  a.x = d->x;
+  a.gate = d->gate;
+  a.h0 = d->h0;
+  a.status = status;
+  a.tokens = d->num_tokens;
+  a.seqs = d->num_seqs;
+  a.x_stride = d->x_stride;
+  a.gate_stride = d->gate_stride;
+  a.dim = d->dim;
+  a.dtype = d->dtype;
+  const GlrShape sh = glr_shape(d->num_tokens, d->dim);
+  a.lc_log = sh.lc_log;
+  a.range_blocks = 4;
+  return a;
+}
+
+}  // namespace
+
+struct dpi_adamw_s {
+  std::vector<AdamTensor> tensors;
+  std::vector<int64_t> first_chunk;   // [tensors + 1]
+  int32_t bits = 32;
+  const AdamTensor* dev_tensors = nullptr;
+  const AdamChunk* dev_chunks = nullptr;
+};
+
+namespace {
+
+// Tensors checked, and their chunks counted.
+dpi_status check_adamw(const dpi_adamw_tensor* tensors, int32_t n, int32_t bits, int64_t& chunks) {
+  chunks = 0;
+  if (n < 1 || !tensors) return dpi_fail_status(DPI_ERR_INVALID_ARG, "no tensors");
+  if (bits != 32 && bits != 8) return dpi_fail_status(DPI_ERR_INVALID_ARG, "state_bits must be 32 or 8");
+  for (int32_t i = 0; i < n; ++i) {
+    const dpi_adamw_tensor& t = tensors[i];
+    if (t.count < 0) return dpi_fail_status(DPI_ERR_INVALID_ARG, "tensor %d: negative count", i);
+    if (!known_dtype(t.param_dtype) || !known_dtype(t.grad_dtype))
+      return dpi_fail_status(DPI_ERR_INVALID_ARG, "tensor %d: bad dtype", i);
+    if (t.count > 0 && (!t.param || !t.m || !t.v)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "tensor %d: NULL", i);
+    if (bits == 8 && t.count > 0 && (!t.m_scale || !t.v_scale))
+      return dpi_fail_status(DPI_ERR_INVALID_ARG, "tensor %d: 8-bit states without scales", i);
+    if (off_by(t.param, elem_size(t.param_dtype)) || off_by(t.master, 4) || off_by(t.m_scale, 4) || off_by(t.v_scale, 4) ||
+        (bits == 32 && (off_by(t.m, 4) || off_by(t.v, 4))))
+      return dpi_fail_status(DPI_ERR_MISALIGNED, "tensor %d not element-aligned", i);
+    if (t.count > (int64_t(1) << 42)) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "tensor %d too large", i);
+    chunks += (t.count + kAdamChunk - 1) / kAdamChunk;
+    if (chunks > INT32_MAX) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "tensors too large");
+  }
+  return DPI_OK;
+}
+
+size_t adamw_table_bytes(int32_t n) { return ((size_t)n * sizeof(AdamTensor) + 255) & ~size_t(255); }
+
+}  // namespace
+
+extern "C" {
+
+dpi_status dpi_embed_forward(const void* table, int32_t table_dtype, int64_t num_rows, int32_t dim,
+                             const int32_t* ids, int64_t num_tokens, float scale, int32_t padding_id, void* out,
+                             int32_t out_dtype, int64_t out_stride, int32_t* device_status, void* stream) {
+  DPI_TRY(check_sizes(num_rows, dim, num_tokens));
+  if (!known_dtype(table_dtype) || !known_dtype(out_dtype)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "bad dtype");
+  if (num_tokens == 0) return DPI_OK;
+  DPI_TRY(check_rows(table, table_dtype, dim, dim, num_rows, "table"));
+  DPI_TRY(check_rows(out, out_dtype, out_stride, dim, num_tokens, "out"));
+  DPI_TRY(check_words(ids, true, "ids"));
+  DPI_TRY(check_words(device_status, false, "device_status"));
+  EmbedArgs a{};
+  a.table = table;
+  a.ids = ids;
+  a.out = out;
+  a.status = device_status;
+  a.tokens = num_tokens;
+  a.num_rows = num_rows;
+  a.out_stride = out_stride;
+  a.dim = dim;
+  a.table_dtype = table_dtype;
+  a.out_dtype = out_dtype;
+  a.padding_id = padding_id;
+  a.scale = scale;
+  const hipError_t e = launch_embed(a, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "embedding launch");
+}
+
+size_t dpi_embed_workspace_bytes(int64_t num_rows, int32_t dim, int64_t num_tokens) {
+  if (check_sizes(num_rows, dim, num_tokens) != DPI_OK) return 0;
+  return embed_grad_layout(num_rows, dim, num_tokens).bytes;
+}
+
+dpi_status dpi_embed_backward(const void* dout, int32_t dout_dtype, int64_t dout_stride, const int32_t* ids,
+                              int64_t num_tokens, float scale, int32_t padding_id, void* grad, int32_t grad_dtype,
+                              int64_t num_rows, int32_t dim, void* workspace, size_t workspace_bytes,
+                              int32_t* device_status, void* stream) {
+  DPI_TRY(check_sizes(num_rows, dim, num_tokens));
+  if (!known_dtype(dout_dtype) || !known_dtype(grad_dtype)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "bad dtype");
+  DPI_TRY(check_rows(grad, grad_dtype, dim, dim, num_rows, "grad"));
+  DPI_TRY(check_words(device_status, false, "device_status"));
+  EmbedGradArgs a{};
+  if (num_tokens > 0) {
+    DPI_TRY(check_rows(dout, dout_dtype, dout_stride, dim, num_tokens, "dout"));
+    DPI_TRY(check_words(ids, true, "ids"));
+    const EmbedGradLayout L = embed_grad_layout(num_rows, dim, num_tokens);
+    DPI_TRY(check_workspace(workspace, workspace_bytes, L.bytes));
+    char* ws = static_cast<char*>(workspace);
+    for (int k = 0; k < 2; ++k) {
+      a.keys[k] = reinterpret_cast<uint32_t*>(ws + L.keys[k]);
+      a.toks[k] = reinterpret_cast<uint32_t*>(ws + L.toks[k]);
+    }
+    a.hist = reinterpret_cast<uint32_t*>(ws + L.hist);
+    a.total = reinterpret_cast<uint32_t*>(ws + L.total);
+    a.part = reinterpret_cast<float*>(ws + L.part);
+    a.passes = L.passes;
+    a.bits = L.bits;
+  }
+  a.dout = dout;
+  a.ids = ids;
+  a.grad = grad;
+  a.status = device_status;
+  a.tokens = num_tokens;
+  a.num_rows = num_rows;
+  a.dout_stride = dout_stride;
+  a.dim = dim;
+  a.dout_dtype = dout_dtype;
+  a.grad_dtype = grad_dtype;
+  a.padding_id = padding_id;
+  a.scale = scale;
+  const hipError_t e = launch_embed_grad(a, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "embedding gradient launch");
+}
+
+size_t dpi_glr_entry_bytes(const dpi_glr_desc* desc) {
+  if (check_glr(desc) != DPI_OK) return 0;
+  return std::max<size_t>(16, (size_t)glr_shape(desc->num_tokens, desc->dim).blocks * (size_t)desc->dim * sizeof(float));
+}
+
+size_t dpi_glr_workspace_bytes(const dpi_glr_desc* desc) {
+  if (check_glr(desc) != DPI_OK) return 0;
+  return 16;
+}
+
+dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, float* h_last, void* entry,
+                           void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream) {
+  DPI_TRY(check_glr(desc));
+  DPI_TRY(check_glr_operands(desc));
+  DPI_TRY(check_rows(h, desc->dtype, h_stride, desc->dim, desc->num_tokens, "h"));
+  DPI_TRY(check_words(h_last, false, "h_last"));
+  DPI_TRY(check_words(entry, false, "entry"));
+  DPI_TRY(check_words(device_status, false, "device_status"));
+  DPI_TRY(check_workspace(workspace, workspace_bytes, dpi_glr_workspace_bytes(desc)));
+  GlrArgs a = glr_args(desc, device_status);
+  a.h = h;
+  a.h_stride = h_stride;
+  a.h_last = h_last;
+  a.entry = static_cast<float*>(entry);
+  Wide w(desc->dtype, desc->dim);
+  w.add(desc->x, desc->x_stride);
+  w.add(desc->gate, desc->gate_stride);
+  w.add(h, h_stride);
+  a.wide = w.ok;
+  const hipError_t e = launch_glr_forward(a, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "recurrence launch");
+}
+
+dpi_status dpi_glr_backward(const dpi_glr_desc* desc, const void* entry, const void* dh, int64_t dh_stride,
+                            const float* dh_last, void* dx, int64_t dx_stride, void* dgate, int64_t dgate_stride,
+                            float* dh0, void* workspace, size_t workspace_bytes, int32_t* device_status,
+                            void* stream) {
+  DPI_TRY(check_glr(desc));
+  DPI_TRY(check_glr_operands(desc));
+  if (dh) DPI_TRY(check_rows(dh, desc->dtype, dh_stride, desc->dim, desc->num_tokens, "dh"));
+  DPI_TRY(check_rows(dx, desc->dtype, dx_stride, desc->dim, desc->num_tokens, "dx"));
+  DPI_TRY(check_rows(dgate, desc->dtype, dgate_stride, desc->dim, desc->num_tokens, "dgate"));
+  DPI_TRY(check_words(entry, desc->num_tokens > 0, "entry"));
+  DPI_TRY(check_words(dh_last, false, "dh_last"));
+  DPI_TRY(check_words(dh0, false, "dh0"));
+  DPI_TRY(check_words(device_status, false, "device_status"));
+  DPI_TRY(check_workspace(workspace, workspace_bytes, dpi_glr_workspace_bytes(desc)));
+  GlrArgs a = glr_args(desc, device_status);
+  a.entry = static_cast<float*>(const_cast<void*>(entry));
+  a.dh = dh;
+  a.dh_stride = dh_stride;
+  a.dh_last = dh_last;
+  a.dx = dx;
+  a.dx_stride = dx_stride;
+  a.dgate = dgate;
+  a.dgate_stride = dgate_stride;
+  a.dh0 = dh0;
+  Wide w(desc->dtype, desc->dim);
+  w.add(desc->x, desc->x_stride);
+  w.add(desc->gate, desc->gate_stride);
+  if (dh) w.add(dh, dh_stride);
+  w.add(dx, dx_stride);
+  w.add(dgate, dgate_stride);
+  a.wide = w.ok;
+  const hipError_t e = launch_glr_backward(a, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "recurrence gradient launch");
+}
+
+dpi_status dpi_glr_step(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, int32_t dtype,
+                        int64_t batch, int32_t dim, float* state, int64_t num_slots, const int32_t* slots, void* h,
+                        int64_t h_stride, int32_t* device_status, void* stream) {
+  DPI_TRY(check_sizes(num_slots, dim, batch));
+  if (!known_dtype(dtype)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "bad dtype");
+  if (batch == 0) return DPI_OK;
+  DPI_TRY(check_rows(x, dtype, x_stride, dim, batch, "x"));
+  DPI_TRY(check_rows(gate, dtype, gate_stride, dim, batch, "gate"));
+  DPI_TRY(check_rows(h, dtype, h_stride, dim, batch, "h"));
+  DPI_TRY(check_words(state, num_slots > 0, "state"));
+  DPI_TRY(check_words(slots, false, "slots"));
+  DPI_TRY(check_words(device_status, false, "device_status"));
+  GlrStepArgs a{};
+  a.x = x;
+  a.gate = gate;
+  a.state = state;
+  a.slots = slots;
+  a.h = h;
+  a.status = device_status;
+  a.batch = batch;
+  a.num_slots = num_slots;
+  a.x_stride = x_stride;
+  a.gate_stride = gate_stride;
+  a.h_stride = h_stride;
+  a.dim = dim;
+  a.dtype = dtype;
+  Wide w(dtype, dim);
+  w.add(x, x_stride);
+  w.add(gate, gate_stride);
+  w.add(h, h_stride);
+  a.wide = w.ok && !off_by(state, 16);
+  const hipError_t e = launch_glr_step(a, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "recurrence step launch");
+}
+
+size_t dpi_adamw_workspace_bytes(const dpi_adamw_tensor* tensors, int32_t num_tensors, int32_t state_bits) {
+  int64_t chunks = 0;
+  if (check_adamw(tensors, num_tensors, state_bits, chunks) != DPI_OK) return 0;
+  return adamw_table_bytes(num_tensors) + std::max<size_t>(16, (size_t)chunks * sizeof(AdamChunk));
+}
+
+dpi_status dpi_adamw_create(const dpi_adamw_tensor* tensors, int32_t num_tensors, int32_t state_bits,
+                            void* workspace, size_t workspace_bytes, dpi_adamw_t* out) {
+  if (!out) return dpi_fail_status(DPI_ERR_INVALID_ARG, "out is NULL");
+  *out = nullptr;
+  int64_t chunks = 0;
+  DPI_TRY(check_adamw(tensors, num_tensors, state_bits, chunks));
+  DPI_TRY(check_workspace(workspace, workspace_bytes, dpi_adamw_workspace_bytes(tensors, num_tensors, state_bits)));
+  dpi_adamw_s* h = nullptr;
+  try {
+    h = new dpi_adamw_s();
+    std::vector<AdamChunk> map;
+    map.reserve((size_t)chunks);
+    h->tensors.reserve((size_t)num_tensors);
+    h->first_chunk.reserve((size_t)num_tensors + 1);
+    for (int32_t i = 0; i < num_tensors; ++i) {
+      const dpi_adamw_tensor& t = tensors[i];
+      h->tensors.push_back(AdamTensor{t.param, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, t.param_dtype, t.grad_dtype});
+      h->first_chunk.push_back((int64_t)map.size());
+      for (int64_t c = 0; c * kAdamChunk < t.count; ++c) map.push_back(AdamChunk{i, (int32_t)c});
+    }
+    h->first_chunk.push_back((int64_t)map.size());
+    h->bits = state_bits;
+    char* ws = static_cast<char*>(workspace);
+    h->dev_tensors = reinterpret_cast<const AdamTensor*>(ws);
+    h->dev_chunks = reinterpret_cast<const AdamChunk*>(ws + adamw_table_bytes(num_tensors));
+    hipError_t e = hipMemcpy(ws, h->tensors.data(), h->tensors.size() * sizeof(AdamTensor), hipMemcpyHostToDevice);
+    if (e == hipSuccess && !map.empty())
+      e = hipMemcpy(ws + adamw_table_bytes(num_tensors), map.data(), map.size() * sizeof(AdamChunk), hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+      delete h;
+      return dpi_hip_status(e, "copy of the tensors' description");
+    }
+  } catch (const std::bad_alloc&) {
+    delete h;
+    return dpi_fail_status(DPI_ERR_INVALID_ARG, "out of host memory");
+  }
+  *out = h;
+  return DPI_OK;
+}
+
+dpi_status dpi_adamw_step(dpi_adamw_t adamw, const void* const* grads, const dpi_adamw_hyper* hyper, void* stream) {
+  if (!adamw) return dpi_fail_status(DPI_ERR_INVALID_ARG, "adamw is NULL");
+  if (!grads || !hyper) return dpi_fail_status(DPI_ERR_INVALID_ARG, "grads or hyper is NULL");
+  const dpi_adamw_hyper& y = *hyper;
+  const auto not_in = [](double v, double lo, double hi) { return !(v >= lo && v < hi); };   // true for a NaN
+  if (not_in(y.lr, 0, HUGE_VAL) || not_in(y.weight_decay, 0, HUGE_VAL) || not_in(y.eps, 0, HUGE_VAL))
+    return dpi_fail_status(DPI_ERR_INVALID_ARG, "lr, weight_decay and eps must be finite and >= 0");
+  if (not_in(y.beta1, 0, 1) || not_in(y.beta2, 0, 1)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "betas must lie in [0, 1)");
+  if (y.step < 1) return dpi_fail_status(DPI_ERR_INVALID_ARG, "step must be >= 1");
+  if (!std::isfinite(y.grad_scale)) return dpi_fail_status(DPI_ERR_INVALID_ARG, "grad_scale is not finite");
+  const int32_t n = (int32_t)adamw->tensors.size();
+  for (int32_t i = 0; i < n; ++i)
+    if (off_by(grads[i], elem_size(adamw->tensors[i].grad_dtype)))
+      return dpi_fail_status(DPI_ERR_MISALIGNED, "gradient %d not element-aligned", i);
+  AdamArgs a{};
+  a.tensors = adamw->dev_tensors;
+  a.chunks = adamw->dev_chunks;
+  a.bits8 = adamw->bits == 8;
+  a.beta1 = (float)y.beta1;
+  a.beta2 = (float)y.beta2;
+  a.omb1 = (float)(1.0 - y.beta1);
+  a.omb2 = (float)(1.0 - y.beta2);
+  a.eps = (float)y.eps;
+  a.step_size = (float)(y.lr / (1.0 - std::pow(y.beta1, (double)y.step)));
+  a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(y.beta2, (double)y.step)));
+  a.decay = (float)(1.0 - y.lr * y.weight_decay);
+  a.grad_scale = (float)y.grad_scale;
+  a.seed = y.seed + (uint32_t)(uint64_t)y.step * 0x9E3779B1u;
+  for (int32_t i0 = 0; i0 < n; i0 += kAdamMaxTensors) {
+    const int32_t i1 = std::min(n, i0 + kAdamMaxTensors);
+    a.first_tensor = i0;
+    a.first_chunk = adamw->first_chunk[i0];
+    for (int32_t i = i0; i < i1; ++i) a.grads[i - i0] = grads[i];
+    const hipError_t e = launch_adamw(a, adamw->first_chunk[i1] - a.first_chunk, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return dpi_hip_status(e, "AdamW launch");
+  }
+  return DPI_OK;
+}
+
+void dpi_adamw_destroy(dpi_adamw_t adamw) { delete adamw; }
+
+}  // extern "C"

@@ -1,0 +1,137 @@
+// Arguments of the behaviour-sequence kernels (embed.hip, recur.hip) and of the
+// optimiser's (adamw.hip), filled and checked by seq_api.cpp.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "dpi.h"
+
+namespace dpi {
+
+// ---------------------------------------------------------------- embedding
+struct EmbedArgs {
+  const void* table;
+  const int32_t* ids;
+  void* out;
+  int32_t* status;
+  int64_t tokens, num_rows, out_stride;
+  int32_t dim, table_dtype, out_dtype, padding_id;
+  float scale;
+};
+
+// Tokens sorted by id for the gradient: least significant digit first, two
+// ping-pong pairs of key and token arrays.
+constexpr int kSortThreads = 256;
+constexpr int kSortItems = 16;                              // items per thread
+constexpr int kSortTile = kSortThreads * kSortItems;        // items per block
+constexpr int kSortMaxBits = 8;                             // bits of a digit
+constexpr int kSumChunk = 64;                               // sorted tokens summed by one group of lanes
+
+struct EmbedGradArgs {
+  const void* dout;
+  const int32_t* ids;
+  void* grad;
+  int32_t* status;
+  int64_t tokens, num_rows, dout_stride;
+  int32_t dim, dout_dtype, grad_dtype, padding_id;
+  float scale;
+  // workspace
+  uint32_t* keys[2];
+  uint32_t* toks[2];
+  uint32_t* hist;      // [bins][tiles]
+  uint32_t* total;     // [bins]
+  float* part;         // [chunks][2][dim]: a chunk's part of a row that began before it, of one that goes on after it
+  int32_t passes, bits;
+};
+
+struct EmbedGradLayout {
+  int32_t passes, bits;
+  int64_t tiles, chunks;
+  size_t keys[2], toks[2], hist, total, part, bytes;
+};
+EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens);
+
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t s);
+hipError_t launch_embed_grad(const EmbedGradArgs& a, hipStream_t s);
+
+// --------------------------------------------------------------- recurrence
+struct GlrArgs {
+  const int32_t* offsets;
+  const void* x;
+  const void* gate;
+  const float* h0;        // or nullptr
+  void* h;                // forward
+  float* h_last;          // forward, or nullptr
+  float* entry;           // [blocks][dim]: the state that enters a block of tokens (forward: or nullptr)
+  const void* dh;         // backward, or nullptr
+  const float* dh_last;   // backward, or nullptr
+  void* dx;
+  void* dgate;
+  float* dh0;             // backward, or nullptr
+  int32_t* status;
+  int64_t tokens, seqs;
+  int64_t x_stride, gate_stride, h_stride, dh_stride, dx_stride, dgate_stride;
+  int32_t dim, dtype;
+  int32_t wide;           // every row is aligned to a thread's whole access
+  int32_t lc_log;         // log2 of the lanes that cover a block of channels
+  int32_t range_blocks;   // blocks of tokens whose sequences a workgroup takes
+};
+
+constexpr int kGlrThreads = 256;
+constexpr int kGlrV = 4;   // channels per thread
+constexpr int kGlrK = 8;   // tokens per thread
+
+struct GlrShape {
+  int32_t lc_log;
+  int64_t block_tokens, blocks, channel_blocks;
+};
+GlrShape glr_shape(int64_t tokens, int32_t dim);
+
+hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s);
+hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s);
+
+struct GlrStepArgs {
+  const void* x;
+  const void* gate;
+  float* state;
+  const int32_t* slots;   // or nullptr: row b's state is row b
+  void* h;
+  int32_t* status;
+  int64_t batch, num_slots, x_stride, gate_stride, h_stride;
+  int32_t dim, dtype, wide;
+};
+hipError_t launch_glr_step(const GlrStepArgs& a, hipStream_t s);
+
+// -------------------------------------------------------------------- AdamW
+constexpr int kAdamBlock = 256;        // elements that share a scale of an 8-bit state
+constexpr int kAdamChunk = 4096;       // elements a workgroup takes: of one tensor
+constexpr int kAdamMaxTensors = 256;   // tensors of one launch (their gradients' addresses are kernel arguments)
+
+struct AdamTensor {
+  void* param;
+  float* master;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int64_t count;
+  int32_t param_dtype, grad_dtype;
+};
+
+struct AdamChunk {
+  int32_t tensor, chunk;
+};
+
+struct AdamArgs {
+  const AdamTensor* tensors;
+  const AdamChunk* chunks;
+  int64_t first_chunk;
+  int32_t first_tensor, bits8;
+  float beta1, beta2, omb1, omb2, eps, step_size, root, decay, grad_scale;
+  uint32_t seed;
+  const void* grads[kAdamMaxTensors];
+};
+hipError_t launch_adamw(const AdamArgs& a, int64_t chunks, hipStream_t s);
+
+}  // namespace dpi

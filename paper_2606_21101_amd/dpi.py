@@ -26,6 +26,7 @@ DPI_ERR_HIP = 7
 
 DPI_F32 = 0
 DPI_F16 = 1
+DPI_BF16 = 2
 DPI_X_F32 = 0
 DPI_X_I64 = 1
 DPI_X_I32 = 2
@@ -43,6 +44,7 @@ DPI_MAX_DIM = 65536
 DPI_NOALLOC_SCRATCH_BYTES = 64 << 20
 DPI_DEVSTAT_BAD_OFFSETS = 1
 DPI_DEVSTAT_BAD_ID = 2
+DPI_ADAMW_BLOCK = 256
 
 
 class dpi_table_meta(ctypes.Structure):
@@ -66,6 +68,25 @@ class dpi_dcn_desc(ctypes.Structure):
                 ("n_mlp", ctypes.c_int32), ("mlp_dims", ctypes.POINTER(ctypes.c_int32)),
                 ("cross_w", ctypes.POINTER(ctypes.c_void_p)), ("cross_b", ctypes.POINTER(ctypes.c_void_p)),
                 ("mlp_w", ctypes.POINTER(ctypes.c_void_p)), ("mlp_b", ctypes.POINTER(ctypes.c_void_p))]
+
+
+class dpi_glr_desc(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("num_seqs", ctypes.c_int64), ("dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("max_len", ctypes.c_int64), ("offsets", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("x_stride", ctypes.c_int64),
+                ("gate_stride", ctypes.c_int64), ("h0", ctypes.c_void_p)]
+
+
+class dpi_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("count", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class dpi_adamw_hyper(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("grad_scale", ctypes.c_double),
+                ("step", ctypes.c_int64), ("seed", ctypes.c_uint32)]
 
 
 class DpiError(RuntimeError):
@@ -133,6 +154,31 @@ def load() -> ctypes.CDLL:
     lib.dpi_lookup_noalloc.restype = ctypes.c_int
     lib.dpi_lookup_noalloc.argtypes = [ctypes.POINTER(dpi_table_meta), i32, ctypes.POINTER(vp), vp, vp, i64, i64,
                                        ctypes.POINTER(i32), ctypes.POINTER(dpi_plan_opts), vp, vp, vp]
+    f32, desc, hyper = ctypes.c_float, ctypes.POINTER(dpi_glr_desc), ctypes.POINTER(dpi_adamw_hyper)
+    lib.dpi_embed_forward.restype = ctypes.c_int
+    lib.dpi_embed_forward.argtypes = [vp, i32, i64, i32, vp, i64, f32, i32, vp, i32, i64, vp, vp]
+    lib.dpi_embed_workspace_bytes.restype = sz
+    lib.dpi_embed_workspace_bytes.argtypes = [i64, i32, i64]
+    lib.dpi_embed_backward.restype = ctypes.c_int
+    lib.dpi_embed_backward.argtypes = [vp, i32, i64, vp, i64, f32, i32, vp, i32, i64, i32, vp, sz, vp, vp]
+    lib.dpi_glr_entry_bytes.restype = sz
+    lib.dpi_glr_entry_bytes.argtypes = [desc]
+    lib.dpi_glr_workspace_bytes.restype = sz
+    lib.dpi_glr_workspace_bytes.argtypes = [desc]
+    lib.dpi_glr_forward.restype = ctypes.c_int
+    lib.dpi_glr_forward.argtypes = [desc, vp, i64, vp, vp, vp, sz, vp, vp]
+    lib.dpi_glr_backward.restype = ctypes.c_int
+    lib.dpi_glr_backward.argtypes = [desc, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp, vp]
+    lib.dpi_glr_step.restype = ctypes.c_int
+    lib.dpi_glr_step.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i64, vp, vp, i64, vp, vp]
+    lib.dpi_adamw_workspace_bytes.restype = sz
+    lib.dpi_adamw_workspace_bytes.argtypes = [ctypes.POINTER(dpi_adamw_tensor), i32, i32]
+    lib.dpi_adamw_create.restype = ctypes.c_int
+    lib.dpi_adamw_create.argtypes = [ctypes.POINTER(dpi_adamw_tensor), i32, i32, vp, sz, ctypes.POINTER(vp)]
+    lib.dpi_adamw_step.restype = ctypes.c_int
+    lib.dpi_adamw_step.argtypes = [vp, ctypes.POINTER(vp), hyper, vp]
+    lib.dpi_adamw_destroy.restype = None
+    lib.dpi_adamw_destroy.argtypes = [vp]
     lib.dpi_plan_destroy.restype = None
     lib.dpi_plan_destroy.argtypes = [vp]
     _lib = lib
@@ -416,3 +462,83 @@ def dpi_plan_destroy(plan: Plan) -> None:
     if plan.handle:
         load().dpi_plan_destroy(ctypes.c_void_p(plan.handle))
         plan.handle = 0
+
+
+def dpi_embed_forward(table, table_dtype: int, num_rows: int, dim: int, ids, num_tokens: int, scale: float,
+                      padding_id: int, out, out_dtype: int, out_stride: int, device_status=None, stream=None) -> None:
+    """out[i] = scale * table[ids[i]], rows of zeros for the padding id."""
+    _check(load().dpi_embed_forward(_ptr(table), table_dtype, num_rows, dim, _ptr(ids), num_tokens, scale, padding_id,
+                                    _ptr(out), out_dtype, out_stride, _ptr(device_status), _stream(stream)))
+
+
+def dpi_embed_workspace_bytes(num_rows: int, dim: int, num_tokens: int) -> int:
+    return int(load().dpi_embed_workspace_bytes(num_rows, dim, num_tokens))
+
+
+def dpi_embed_backward(dout, dout_dtype: int, dout_stride: int, ids, num_tokens: int, scale: float, padding_id: int,
+                       grad, grad_dtype: int, num_rows: int, dim: int, workspace,
+                       workspace_bytes: Optional[int] = None, device_status=None, stream=None) -> None:
+    """The table's gradient of dpi_embed_forward (every element written)."""
+    if workspace_bytes is None:
+        workspace_bytes = int(workspace.numel() * workspace.element_size())
+    _check(load().dpi_embed_backward(_ptr(dout), dout_dtype, dout_stride, _ptr(ids), num_tokens, scale, padding_id,
+                                     _ptr(grad), grad_dtype, num_rows, dim, _ptr(workspace), workspace_bytes,
+                                     _ptr(device_status), _stream(stream)))
+
+
+def dpi_glr_entry_bytes(desc: dpi_glr_desc) -> int:
+    return int(load().dpi_glr_entry_bytes(ctypes.byref(desc)))
+
+
+def dpi_glr_workspace_bytes(desc: dpi_glr_desc) -> int:
+    return int(load().dpi_glr_workspace_bytes(ctypes.byref(desc)))
+
+
+def dpi_glr_forward(desc: dpi_glr_desc, h, h_stride: int, h_last, entry, workspace,
+                    workspace_bytes: Optional[int] = None, device_status=None, stream=None) -> None:
+    """Gated linear recurrence over packed sequences."""
+    if workspace_bytes is None:
+        workspace_bytes = int(workspace.numel() * workspace.element_size())
+    _check(load().dpi_glr_forward(ctypes.byref(desc), _ptr(h), h_stride, _ptr(h_last), _ptr(entry), _ptr(workspace),
+                                  workspace_bytes, _ptr(device_status), _stream(stream)))
+
+
+def dpi_glr_backward(desc: dpi_glr_desc, entry, dh, dh_stride: int, dh_last, dx, dx_stride: int, dgate,
+                     dgate_stride: int, dh0, workspace, workspace_bytes: Optional[int] = None, device_status=None,
+                     stream=None) -> None:
+    """Its gradients, from what the forward pass over the same desc saved in `entry`."""
+    if workspace_bytes is None:
+        workspace_bytes = int(workspace.numel() * workspace.element_size())
+    _check(load().dpi_glr_backward(ctypes.byref(desc), _ptr(entry), _ptr(dh), dh_stride, _ptr(dh_last), _ptr(dx),
+                                   dx_stride, _ptr(dgate), dgate_stride, _ptr(dh0), _ptr(workspace), workspace_bytes,
+                                   _ptr(device_status), _stream(stream)))
+
+
+def dpi_glr_step(x, x_stride: int, gate, gate_stride: int, dtype: int, batch: int, dim: int, state, num_slots: int,
+                 slots, h, h_stride: int, device_status=None, stream=None) -> None:
+    """One token for each of `batch` sequences whose states lie in a store."""
+    _check(load().dpi_glr_step(_ptr(x), x_stride, _ptr(gate), gate_stride, dtype, batch, dim, _ptr(state), num_slots,
+                               _ptr(slots), _ptr(h), h_stride, _ptr(device_status), _stream(stream)))
+
+
+def dpi_adamw_workspace_bytes(tensors, state_bits: int) -> int:
+    return int(load().dpi_adamw_workspace_bytes(tensors, len(tensors), state_bits))
+
+
+def dpi_adamw_create(tensors, state_bits: int, workspace, workspace_bytes: Optional[int] = None) -> int:
+    """tensors: ctypes array of dpi_adamw_tensor.  Returns the handle (dpi_adamw_destroy frees it)."""
+    if workspace_bytes is None:
+        workspace_bytes = int(workspace.numel() * workspace.element_size())
+    out = ctypes.c_void_p()
+    _check(load().dpi_adamw_create(tensors, len(tensors), state_bits, _ptr(workspace), workspace_bytes,
+                                   ctypes.byref(out)))
+    return out.value
+
+
+def dpi_adamw_step(handle: int, grads, hyper: dpi_adamw_hyper, stream=None) -> None:
+    """grads: ctypes array of the gradients' device pointers."""
+    _check(load().dpi_adamw_step(handle, grads, ctypes.byref(hyper), _stream(stream)))
+
+
+def dpi_adamw_destroy(handle: int) -> None:
+    load().dpi_adamw_destroy(handle)

@@ -1,0 +1,138 @@
+"""AdamW over many tensors in one launch, with states in 32 bits or in 8.
+
+``AdamW`` keeps the parameters, their states and, for parameters of 16 bits that
+ask for it, float32 master copies; ``step`` updates them in place on the current
+(or given) stream.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence
+
+import torch
+
+from . import dpi
+from .sequence import _DT, _dtype, _here, _on, _refuse
+
+
+class AdamW:
+    """params: contiguous tensors on one GPU.  masters: True for float32 copies of
+    all of them, a list of such copies, or None.  state_bits 8: m and v are e4m3
+    values with a float32 scale for every 256 elements (m_scale, v_scale), rounded
+    at random from `seed`, the step and the element.  m, v, m_scale, v_scale: the
+    states to go on from (lists of tensors, updated in place), zeros without."""
+
+    def __init__(self, params: Sequence[torch.Tensor], masters=None, state_bits: int = 32, m=None, v=None,
+                 m_scale=None, v_scale=None, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 0.01, seed: int = 0):
+        self.params = list(params)
+        if not self.params:
+            _refuse("no parameters")
+        if state_bits not in (8, 32):
+            _refuse("state_bits must be 32 or 8")
+        self.device = self.params[0].device
+        self.state_bits, self.step_count = state_bits, 0
+        self.lr, self.betas, self.eps, self.weight_decay, self.seed = lr, tuple(betas), eps, weight_decay, seed
+        if masters is True:
+            masters = [p.detach().to(torch.float32, copy=True) for p in self.params]
+        self.masters = list(masters) if masters else None
+        held = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        blocks = [-(-p.numel() // dpi.DPI_ADAMW_BLOCK) for p in self.params]
+        self.m = list(m) if m is not None else [torch.zeros_like(p, dtype=held) for p in self.params]
+        self.v = list(v) if v is not None else [torch.zeros_like(p, dtype=held) for p in self.params]
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            def scales():
+                return [torch.zeros(b, dtype=torch.float32, device=self.device) for b in blocks]
+            self.m_scale = list(m_scale) if m_scale is not None else scales()
+            self.v_scale = list(v_scale) if v_scale is not None else scales()
+        self._check(held, blocks)
+        self._grad_dtypes = None
+        self._handle = None
+
+    def _check(self, held, blocks) -> None:
+        for i, p in enumerate(self.params):
+            if p.dtype not in _DT or not p.is_contiguous():
+                _refuse(f"parameter {i} must be contiguous, of float32, float16 or bfloat16")
+            like = [("m", self.m, held), ("v", self.v, held)]
+            if self.masters is not None:
+                like.append(("masters", self.masters, torch.float32))
+            for what, tensors, dtype in like:
+                if len(tensors) != len(self.params):
+                    _refuse(f"{what}: one tensor a parameter")
+                t = tensors[i]
+                if t.dtype != dtype or t.shape != p.shape or not t.is_contiguous():
+                    _refuse(f"{what}[{i}] must be contiguous {dtype} of the parameter's shape")
+                if t.device != self.device:
+                    _refuse(f"{what}[{i}] is not on {self.device}")
+            if p.device != self.device:
+                _refuse(f"parameter {i} is not on {self.device}")
+            if self.state_bits == 8:
+                for what, tensors in (("m_scale", self.m_scale), ("v_scale", self.v_scale)):
+                    if len(tensors) != len(self.params):
+                        _refuse(f"{what}: one tensor a parameter")
+                    t = tensors[i]
+                    if t.dtype != torch.float32 or t.numel() != blocks[i] or not t.is_contiguous() or t.device != self.device:
+                        _refuse(f"{what}[{i}] must be {blocks[i]} contiguous float32 on {self.device}")
+
+    def _create(self, grad_dtypes) -> None:
+        """The library's handle over these tensors (made anew when the gradients' dtypes change)."""
+        torch.cuda.synchronize(self.device)   # a step in flight reads the description that is replaced
+        self._destroy()
+        n = len(self.params)
+        arr = (dpi.dpi_adamw_tensor * n)()
+        for i, p in enumerate(self.params):
+            arr[i] = dpi.dpi_adamw_tensor(
+                p.data_ptr(), self.masters[i].data_ptr() if self.masters else None, self.m[i].data_ptr(),
+                self.v[i].data_ptr(), self.m_scale[i].data_ptr() if self.m_scale else None,
+                self.v_scale[i].data_ptr() if self.v_scale else None, p.numel(), _DT[p.dtype], _DT[grad_dtypes[i]])
+        need = dpi.dpi_adamw_workspace_bytes(arr, self.state_bits)
+        if need == 0:
+            raise dpi.DpiError(dpi.DPI_ERR_INVALID_ARG, dpi.dpi_last_error())
+        self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        torch.cuda.synchronize(self.device)   # ... and its memory may have been another tensor's until now
+        self._handle = dpi.dpi_adamw_create(arr, self.state_bits, self._ws)
+        self._grad_dtypes = grad_dtypes
+        self._counts = [p.numel() for p in self.params]
+        self._grads = (ctypes.c_void_p * n)()
+
+    def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, step: Optional[int] = None,
+             lr: Optional[float] = None, grad_scale: float = 1.0, stream=None) -> None:
+        """One step from `grads` (the parameters' .grad when None; a None among them leaves its parameter as it
+        is).  step: the step's number t >= 1 (one more than the last when None)."""
+        if grads is None:
+            grads = [p.grad for p in self.params]
+        if len(grads) != len(self.params):
+            _refuse("one gradient a parameter")
+        _here(self.device)
+        held = self._grad_dtypes or [p.dtype for p in self.params]
+        dtypes = [g.dtype if g is not None else d for g, d in zip(grads, held)]
+        if dtypes != self._grad_dtypes:
+            for g in grads:
+                if g is not None:
+                    _dtype(g, "gradient")
+            self._create(dtypes)
+        for i, (g, n) in enumerate(zip(grads, self._counts)):
+            if g is None:
+                self._grads[i] = None
+                continue
+            if g.numel() != n or g.device != self.device or not g.is_contiguous():
+                _refuse(f"gradient {i} must be contiguous, of the parameter's size, on {self.device}")
+            self._grads[i] = g.data_ptr()
+        t = self.step_count + 1 if step is None else int(step)
+        hyper = dpi.dpi_adamw_hyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps,
+                                    self.weight_decay, grad_scale, t, self.seed & 0xFFFFFFFF)
+        handle, _ = _on(stream)
+        if stream is not None:
+            self._ws.record_stream(torch.cuda.ExternalStream(handle))
+        dpi.dpi_adamw_step(self._handle, self._grads, hyper, handle)
+        self.step_count = t
+
+    def _destroy(self) -> None:
+        if getattr(self, "_handle", None):
+            dpi.dpi_adamw_destroy(self._handle)
+            self._handle = None
+
+    def __del__(self):
+        if dpi._lib is not None:
+            self._destroy()

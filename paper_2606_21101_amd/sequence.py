@@ -1,0 +1,284 @@
+"""Behaviour sequences: scaled embedding rows and a gated linear recurrence, trained and served.
+
+Histories are packed: the tokens of all sequences one after the other, int32
+``offsets`` [num_seqs + 1] between them.  ``SequenceEmbedding`` turns ids into
+rows, ``GatedRecurrence`` rows and gates into states; called, both take part in
+autograd, and ``forward`` / ``backward`` are the passes themselves, over buffers
+that the caller keeps.  Everything runs in libdpi.so on the current (or given)
+stream; an object may be used on several streams.
+"""
+from __future__ import annotations
+
+import contextlib
+from dataclasses import dataclass
+from typing import Optional, Tuple
+
+import torch
+
+from . import dpi
+
+_DT = {torch.float32: dpi.DPI_F32, torch.float16: dpi.DPI_F16, torch.bfloat16: dpi.DPI_BF16}
+
+
+def _refuse(what: str):
+    raise dpi.DpiError(dpi.DPI_ERR_INVALID_ARG, what)
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    code = _DT.get(t.dtype)
+    if code is None:
+        _refuse(f"{what}: dtype {t.dtype} is none of float32, float16, bfloat16")
+    return code
+
+
+def _here(device: torch.device, *tensors) -> None:
+    """All of them on `device`, which has to be the current one."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        _refuse(f"{device} is not the current GPU")
+    for t in tensors:
+        if t is not None and t.device != device:
+            _refuse(f"a tensor is on {t.device}, not {device}")
+
+
+def _rows(t: torch.Tensor, n: int, dim: int, what: str) -> int:
+    """Row stride of a [n, dim] tensor with consecutive columns."""
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != dim:
+        _refuse(f"{what}: shape {tuple(t.shape)}, not {(n, dim)}")
+    if dim > 1 and n > 0 and t.stride(1) != 1:
+        _refuse(f"{what}: columns are not consecutive")
+    # one row's stride is never used, and torch gives it any value
+    return t.stride(0) if n > 1 else dim
+
+
+def _index(t: torch.Tensor, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        _refuse(f"{what} must be a contiguous vector of int32")
+    return t
+
+
+def _states(t: Optional[torch.Tensor], n: int, dim: int, what: str) -> Optional[torch.Tensor]:
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (n, dim) or not t.is_contiguous()):
+        _refuse(f"{what} must be contiguous float32 {(n, dim)}")
+    return t
+
+
+def _on(stream):
+    """The stream to use, and the context in which its memory is allocated."""
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream, contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream)
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+class _Workspaces:
+    """Device scratch, one buffer a stream: calls on different streams share none."""
+
+    def __init__(self):
+        self._held = {}
+
+    def get(self, stream: int, need: int, device) -> torch.Tensor:
+        ws = self._held.get(stream)
+        if ws is None or ws.numel() < need:
+            ws = self._held[stream] = torch.empty(need, dtype=torch.uint8, device=device)
+        return ws
+
+
+class SequenceEmbedding:
+    """Rows of `table` [num_rows, dim] for lists of token ids, times `scale`.
+
+    A token whose id is `padding_id` (negative: none) has a row of zeros and no
+    part in the gradient; so has an id outside the table, which is also reported
+    in `status`, an int32 tensor of the caller's into which DPI_DEVSTAT_BAD_ID is
+    ORed."""
+
+    def __init__(self, table: torch.Tensor, scale: float = 1.0, padding_id: int = -1,
+                 out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None):
+        if table.dim() != 2 or not table.is_contiguous():
+            _refuse("table must be a contiguous [num_rows, dim] tensor")
+        self.table, self.scale, self.padding_id, self.status = table, float(scale), int(padding_id), status
+        self.num_rows, self.dim = int(table.shape[0]), int(table.shape[1])
+        self.out_dtype = out_dtype if out_dtype is not None else table.dtype
+        self._code = _dtype(table, "table")
+        if self.out_dtype not in _DT:
+            _refuse(f"out_dtype {self.out_dtype}")
+        self._ws = _Workspaces()
+
+    def forward(self, ids: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """[tokens, dim] rows of out_dtype (into `out` when given)."""
+        n = _index(ids, "ids").numel()
+        handle, context = _on(stream)
+        if out is None:
+            with context:
+                out = torch.empty((n, self.dim), dtype=self.out_dtype, device=self.table.device)
+        _here(self.table.device, ids, out, self.status)
+        if out.dtype != self.out_dtype:
+            _refuse(f"out: dtype {out.dtype}, not {self.out_dtype}")
+        dpi.dpi_embed_forward(self.table, self._code, self.num_rows, self.dim, ids, n, self.scale, self.padding_id,
+                              out, _DT[self.out_dtype], _rows(out, n, self.dim, "out"), self.status, handle)
+        return out
+
+    def backward(self, ids: torch.Tensor, dout: torch.Tensor, grad: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+        """The table's gradient [num_rows, dim] from the rows' gradients: of the
+        table's dtype, or of `grad`'s, which is overwritten."""
+        n = _index(ids, "ids").numel()
+        handle, context = _on(stream)
+        with context:
+            if grad is None:
+                grad = torch.empty_like(self.table)
+            ws = self._ws.get(handle, dpi.dpi_embed_workspace_bytes(self.num_rows, self.dim, n), self.table.device)
+        _here(self.table.device, ids, dout, grad, self.status)
+        if tuple(grad.shape) != (self.num_rows, self.dim) or not grad.is_contiguous():
+            _refuse(f"grad must be a contiguous {(self.num_rows, self.dim)} tensor")
+        dpi.dpi_embed_backward(dout, _dtype(dout, "dout"), _rows(dout, n, self.dim, "dout"), ids, n, self.scale,
+                               self.padding_id, grad, _dtype(grad, "grad"), self.num_rows, self.dim, ws, None,
+                               self.status, handle)
+        return grad
+
+    def __call__(self, ids: torch.Tensor) -> torch.Tensor:
+        return _EmbedFn.apply(self.table, ids, self)
+
+
+class _EmbedFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, op):
+        ctx.op = op
+        ctx.save_for_backward(ids)
+        return op.forward(ids)
+
+    @staticmethod
+    def backward(ctx, dout):
+        (ids,) = ctx.saved_tensors
+        if dout.stride(-1) != 1 or dout.stride(0) < dout.shape[1]:
+            dout = dout.contiguous()
+        return ctx.op.backward(ids, dout), None, None
+
+
+@dataclass
+class Saved:
+    """What a backward pass needs of its forward pass: the inputs, unchanged, and the blocks' entry states."""
+    x: torch.Tensor
+    gate: torch.Tensor
+    offsets: torch.Tensor
+    h0: Optional[torch.Tensor]
+    entry: torch.Tensor
+
+
+class GatedRecurrence:
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t with a_t = sigmoid(gate_t), for every channel of every packed sequence.
+
+    x and gate are [tokens, dim] tensors of one dtype; they may be column blocks
+    of a wider tensor.  States that pass between calls (h0, h_last, a store) are
+    float32 [num_seqs, dim].  max_len: a bound on the sequences' lengths (0: none
+    known); it sets how the work is split, not the result."""
+
+    def __init__(self, dim: int, max_len: int = 0, status: Optional[torch.Tensor] = None):
+        self.dim, self.max_len, self.status = int(dim), int(max_len), status
+        self._ws = _Workspaces()
+
+    def _desc(self, x, gate, offsets, h0) -> dpi.dpi_glr_desc:
+        n, seqs = int(x.shape[0]), int(_index(offsets, "offsets").numel()) - 1
+        if seqs < 0:
+            _refuse("offsets must have num_seqs + 1 entries")
+        if gate.dtype != x.dtype:
+            _refuse("x and gate must have one dtype")
+        _states(h0, seqs, self.dim, "h0")
+        return dpi.dpi_glr_desc(n, seqs, self.dim, _dtype(x, "x"), self.max_len, offsets.data_ptr(), x.data_ptr(),
+                                gate.data_ptr(), _rows(x, n, self.dim, "x"), _rows(gate, n, self.dim, "gate"),
+                                None if h0 is None else h0.data_ptr())
+
+    def forward(self, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, h0: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, save: bool = False,
+                stream=None) -> Tuple[torch.Tensor, torch.Tensor, Optional[Saved]]:
+        """States of every token (into `out` when given), each sequence's last state, and, with `save`, what
+        backward() takes."""
+        desc = self._desc(x, gate, offsets, h0)
+        handle, context = _on(stream)
+        with context:
+            if out is None:
+                out = torch.empty((desc.num_tokens, self.dim), dtype=x.dtype, device=x.device)
+            h_last = torch.empty((desc.num_seqs, self.dim), dtype=torch.float32, device=x.device)
+            entry = torch.empty(dpi.dpi_glr_entry_bytes(desc) // 4, dtype=torch.float32, device=x.device) if save else None
+            ws = self._ws.get(handle, dpi.dpi_glr_workspace_bytes(desc), x.device)
+        _here(x.device, gate, offsets, h0, out, self.status)
+        if out.dtype != x.dtype:
+            _refuse("out must have x's dtype")
+        dpi.dpi_glr_forward(desc, out, _rows(out, desc.num_tokens, self.dim, "out"), h_last, entry, ws, None,
+                            self.status, handle)
+        return out, h_last, Saved(x, gate, offsets, h0, entry) if save else None
+
+    def backward(self, saved: Saved, dh: Optional[torch.Tensor], dh_last: Optional[torch.Tensor] = None,
+                 dx: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """Gradients of x, of gate (into `dx`, `dgate` when given) and of h0, from those of the states (dh, of x's
+        dtype) and of the last states (dh_last, float32); either may be None: zeros."""
+        x = saved.x
+        desc = self._desc(x, saved.gate, saved.offsets, saved.h0)
+        n, seqs = desc.num_tokens, desc.num_seqs
+        handle, context = _on(stream)
+        with context:
+            if dx is None:
+                dx = torch.empty((n, self.dim), dtype=x.dtype, device=x.device)
+            if dgate is None:
+                dgate = torch.empty((n, self.dim), dtype=x.dtype, device=x.device)
+            dh0 = torch.empty((seqs, self.dim), dtype=torch.float32, device=x.device)
+            ws = self._ws.get(handle, dpi.dpi_glr_workspace_bytes(desc), x.device)
+        _here(x.device, dh, dh_last, dx, dgate, self.status)
+        for t, what in ((dh, "dh"), (dx, "dx"), (dgate, "dgate")):
+            if t is not None and t.dtype != x.dtype:
+                _refuse(f"{what} must have x's dtype")
+        _states(dh_last, seqs, self.dim, "dh_last")
+        dpi.dpi_glr_backward(desc, saved.entry, dh, 0 if dh is None else _rows(dh, n, self.dim, "dh"), dh_last, dx,
+                             _rows(dx, n, self.dim, "dx"), dgate, _rows(dgate, n, self.dim, "dgate"), dh0, ws, None,
+                             self.status, handle)
+        return dx, dgate, dh0
+
+    def step(self, x: torch.Tensor, gate: torch.Tensor, state: torch.Tensor, slots: Optional[torch.Tensor] = None,
+             out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """One token for each sequence: row b moves row slots[b] (row b without slots) of the store `state`
+        [num_slots, dim] on, in place, and gets it.  Slots must be distinct."""
+        n = int(x.shape[0])
+        if gate.dtype != x.dtype:
+            _refuse("x and gate must have one dtype")
+        if state.dim() != 2:
+            _refuse("state must be a [num_slots, dim] tensor")
+        _states(state, state.shape[0], self.dim, "state")
+        if (_index(slots, "slots").numel() if slots is not None else state.shape[0]) < n:
+            _refuse("fewer slots than rows")
+        handle, context = _on(stream)
+        if out is None:
+            with context:
+                out = torch.empty((n, self.dim), dtype=x.dtype, device=x.device)
+        _here(x.device, gate, state, slots, out, self.status)
+        if out.dtype != x.dtype:
+            _refuse("out must have x's dtype")
+        dpi.dpi_glr_step(x, _rows(x, n, self.dim, "x"), gate, _rows(gate, n, self.dim, "gate"), _dtype(x, "x"), n,
+                         self.dim, state, int(state.shape[0]), slots, out, _rows(out, n, self.dim, "out"), self.status,
+                         handle)
+        return out
+
+    def __call__(self, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor,
+                 h0: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """States and last states, differentiable in x, gate and h0."""
+        return _RecurFn.apply(x, gate, offsets, h0, self)
+
+
+class _RecurFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, offsets, h0, op):
+        h, h_last, saved = op.forward(x, gate, offsets, h0, save=True)
+        ctx.op, ctx.with_h0 = op, h0 is not None
+        ctx.save_for_backward(x, gate, offsets, saved.entry, *([h0] if h0 is not None else []))
+        ctx.set_materialize_grads(False)
+        return h, h_last
+
+    @staticmethod
+    def backward(ctx, dh, dh_last):
+        x, gate, offsets, entry, *rest = ctx.saved_tensors
+        if dh is not None and (dh.stride(-1) != 1 or dh.stride(0) < dh.shape[1]):
+            dh = dh.contiguous()
+        if dh_last is not None:
+            dh_last = dh_last.contiguous()
+        dx, dgate, dh0 = ctx.op.backward(Saved(x, gate, offsets, rest[0] if ctx.with_h0 else None, entry), dh, dh_last)
+        return dx, dgate, None, dh0 if ctx.with_h0 else None, None
