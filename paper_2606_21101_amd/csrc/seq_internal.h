@@ -75,18 +75,30 @@ struct GlrArgs {
   int32_t dim, dtype;
   int32_t wide;           // every row is aligned to a thread's whole access
   int32_t lc_log;         // log2 of the lanes that cover a block of channels
-  int32_t range_blocks;   // blocks of tokens whose sequences a workgroup takes
+  int32_t cut;            // ranges cut sequences (else a wave takes whole ones)
+  int64_t range, units;   // tokens of a wave's range, and ranges
+  float* map_a;           // cut: [units][dim], a range's map, then
+  float* map_s;           //      ... the state that enters it
 };
 
 constexpr int kGlrThreads = 256;
-constexpr int kGlrV = 4;   // channels per thread
-constexpr int kGlrK = 8;   // tokens per thread
+constexpr int kGlrV = 4;              // channels per thread
+constexpr int kGlrK = 8;              // tokens per thread
+constexpr int kGlrWaves = 4096;       // waves a pass is split into, while ...
+constexpr int kGlrRangeBlocks = 16;   // ... a range has at most so many blocks
+constexpr int kGlrWholeBlocks = 32;   // the longest sequence that one wave walks, in blocks
 
 struct GlrShape {
   int32_t lc_log;
   int64_t block_tokens, blocks, channel_blocks;
 };
 GlrShape glr_shape(int64_t tokens, int32_t dim);
+
+struct GlrSplit {
+  int32_t cut;
+  int64_t range, units;
+};
+GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len);
 
 hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s);
 hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s);
