@@ -34,7 +34,17 @@ namespace dpi {
 namespace {
 
 constexpr int V = kGlrV, K = kGlrK, kThreads = kGlrThreads, kWaves = kThreads / 64;
-constexpr int kMaxTokens = 64 * K;   // of a block: one lane covers a row
+
+// A wave's part of the workgroup's LDS: the sequences that begin and end at a block's tokens, where marked, and K slots of
+// V channels for each lane.
+struct Place;
+struct Scratch {
+  int32_t *starts_at, *ends_at;
+  float* slots;
+  __device__ __forceinline__ explicit Scratch(const Place& p);
+};
+constexpr int kSlotBytes = K * 64 * V * 4;
+inline size_t scratch_bytes(int64_t block_tokens) { return kWaves * (kSlotBytes + 2 * (size_t)block_tokens * 4); }
 
 // Product in which 0 times anything is 0.
 __device__ __forceinline__ float mul0(float a, float b) {
@@ -197,11 +207,11 @@ __device__ __forceinline__ Place place_of(const GlrArgs& a) {
   return p;
 }
 
-template <bool WIDE, typename T>
-__device__ __forceinline__ Elems<T, V> row_part(const void* base, int64_t stride, int64_t t, const Place& p) {
-  // a thread without channels reads the row's first ones
-  const T* q = static_cast<const T*>(base) + t * stride + (p.have > 0 ? p.ch : 0);
-  return load_elems<WIDE, T, V>(q, p.have > 0 ? p.have : 1);
+__device__ __forceinline__ Scratch::Scratch(const Place& p) {
+  extern __shared__ __align__(16) char lds[];
+  slots = reinterpret_cast<float*>(lds) + p.wave * (kSlotBytes / 4);
+  starts_at = reinterpret_cast<int32_t*>(lds + kWaves * kSlotBytes) + p.wave * 2 * p.tokens;
+  ends_at = starts_at + p.tokens;
 }
 
 __device__ __forceinline__ void put_channels(float* row, const Place& p, const float* v) {
@@ -210,28 +220,109 @@ __device__ __forceinline__ void put_channels(float* row, const Place& p, const f
     if (i < p.have) row[p.ch + i] = v[i];
 }
 
-// x, gate (and dh) of a block's tokens; those outside [lo, hi) as tokens that keep the state (and have no gradient).
-template <bool WIDE, typename T>
-__device__ __forceinline__ void load_block(const GlrArgs& a, const Place& p, int64_t t0, int64_t lo, int64_t hi,
-                                           Elems<T, V>* x, Elems<T, V>* g, Elems<T, V>* d) {
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int64_t t = clamped(t0 + p.mine + k, lo, hi - 1);
-    if (x) x[k] = row_part<WIDE, T>(a.x, a.x_stride, t, p);
-    g[k] = row_part<WIDE, T>(a.gate, a.gate_stride, t, p);
-    if (d) d[k] = row_part<WIDE, T>(a.dh, a.dh_stride, t, p);
+// A wave's place in its span: the block at token t0, whose rows [first, past) belong to the span.
+struct Block {
+  int64_t t0;
+  int32_t first, past;
+  bool whole;
+
+  __device__ __forceinline__ Block(const Place& p, int64_t t, int64_t lo, int64_t hi)
+      : t0(t), first((int32_t)max(lo - t, (int64_t)0)), past((int32_t)min(hi - t, (int64_t)p.tokens)) {
+    whole = first == 0 && past == p.tokens;
   }
-  if (t0 >= lo && t0 + p.tokens <= hi) return;
+  __device__ __forceinline__ bool has(int32_t row) const { return whole || (row >= first && row < past); }
+};
+
+// The block's rows of a [tokens, dim] operand through a buffer descriptor of its rows up to `past`: a thread keeps one
+// 32-bit offset, its k-th row is a scalar one (64-bit addresses of every row took 40 registers more), and rows past the
+// span are not touched.  A block's rows span less than 2^31 bytes (kGlrMaxStride).
+template <bool WIDE, typename T>
+struct Rows {
+  __amdgpu_buffer_rsrc_t rsrc;
+  int32_t stride, lane;   // bytes; of the thread's first row and channel
+  int32_t have;
+
+  __device__ __forceinline__ Rows(const void* p, int64_t row_stride, const Place& at, const Block& b)
+      : stride((int32_t)row_stride * (int32_t)sizeof(T)), have(at.have) {
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        static_cast<char*>(const_cast<void*>(p)) + b.t0 * row_stride * (int64_t)sizeof(T), (short)0, b.past * stride, 0x00020000);
+    // a thread without channels reads the row's first ones
+    lane = at.mine * stride + (at.have > 0 ? at.ch * (int32_t)sizeof(T) : 0);
+  }
+  __device__ __forceinline__ Elems<T, V> get(int k) const {
+    Elems<T, V> e;
+    if constexpr (WIDE) {
+      if constexpr (sizeof(T) * V == 16) {
+        typedef int quad __attribute__((ext_vector_type(4)));
+        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (quad)__builtin_amdgcn_raw_buffer_load_b128(rsrc, lane, k * stride, 0));
+      } else {
+        typedef int pair __attribute__((ext_vector_type(2)));
+        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (pair)__builtin_amdgcn_raw_buffer_load_b64(rsrc, lane, k * stride, 0));
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int32_t at = lane + min(v, max(have, 1) - 1) * (int32_t)sizeof(T);
+        if constexpr (sizeof(T) == 4)
+          e.raw[v] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, k * stride, 0));
+        else
+          e.raw[v] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, k * stride, 0));
+      }
+    }
+    return e;
+  }
+  __device__ __forceinline__ void put(int k, const float* v) const {
+    typename Raw<T, V>::plain r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = (T)v[i];
+    if constexpr (WIDE) {
+      if constexpr (sizeof(T) * V == 16) {
+        typedef int quad __attribute__((ext_vector_type(4)));
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(quad, r), rsrc, lane, k * stride, 0);
+      } else {
+        typedef int pair __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(pair, r), rsrc, lane, k * stride, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (i >= have) continue;
+        const int32_t at = lane + i * (int32_t)sizeof(T);
+        if constexpr (sizeof(T) == 4)
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, (T)r[i]), rsrc, at, k * stride, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, (T)r[i]), rsrc, at, k * stride, 0);
+      }
+    }
+  }
+};
+
+// The thread's rows of one operand; those outside the span are `other`.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load_block(const void* from, int64_t stride, const Place& p, const Block& b, float other,
+                                           Elems<T, V>* e) {
+  const Rows<WIDE, T> rows(from, stride, p, b);
+#pragma unroll
+  for (int k = 0; k < K; ++k) e[k] = rows.get(k);
+  if (b.whole) return;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const int64_t t = t0 + p.mine + k;
-    if (t >= lo && t < hi) continue;
+    if (b.has(p.mine + k)) continue;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      g[k].raw[v] = (T)INFINITY;
-      if (x) x[k].raw[v] = (T)0.f;
-      if (d) d[k].raw[v] = (T)0.f;
-    }
+    for (int v = 0; v < V; ++v) e[k].raw[v] = (T)other;
+  }
+}
+
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load_dh(const GlrArgs& a, const Place& p, const Block& b, Elems<T, V>* d) {
+  if (a.dh) {
+    load_block<WIDE, T>(a.dh, a.dh_stride, p, b, 0.f, d);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) d[k].raw[v] = (T)0.f;
   }
 }
 
@@ -267,44 +358,102 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
   }
 }
 
-// The maps of a thread's tokens, and their composition (A, S): a start's b takes h0 in, and its a becomes 0.
+// A thread's part of a row of states (zeros without them): what a sequence begins (ends) with.
+__device__ __forceinline__ void edge_state(const float* states, const GlrArgs& a, const Place& p, int32_t seq, float* out) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) out[v] = states && v < p.have ? states[(int64_t)seq * a.dim + p.ch + v] : 0.f;
+}
+
+// The edges among a thread's tokens.  The first one's state is in registers, read as soon as the marks are known with the
+// block's other loads; those of further ones (sequences shorter than K tokens) go to the thread's slots in LDS.
+struct Edges {
+  uint32_t mask;
+  int k;               // the token whose edge is in `state`
+  float state[V];
+  const float* extra;  // [K][64][V], the thread's column
+
+  __device__ __forceinline__ void read(const GlrArgs& a, const Place& p, uint32_t m, const int32_t* seqs, const float* from) {
+    mask = m;
+    k = m ? __builtin_ctz(m) : 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = 0.f;
+    if (m && from) edge_state(from, a, p, seqs[p.mine + k], state);
+  }
+  // Not before the last use of what the slots held.
+  __device__ __forceinline__ void read_more(const GlrArgs& a, const Place& p, const int32_t* seqs, const float* from, float* slots) {
+    extra = slots + p.lane * V;
+    for (uint32_t m = mask & (mask - 1); m; m &= m - 1) {
+      const int i = __builtin_ctz(m);
+      float more[V];
+      edge_state(from, a, p, seqs[p.mine + i], more);
+#pragma unroll
+      for (int v = 0; v < V; ++v) slots[(i * 64 + p.lane) * V + v] = more[v];
+    }
+  }
+  __device__ __forceinline__ bool is(int i) const { return mask >> i & 1; }
+  __device__ __forceinline__ void get(int i, float* out) const {
+#pragma unroll
+    for (int v = 0; v < V; ++v) out[v] = i == k ? state[v] : extra[i * 64 * V + v];
+  }
+};
+
+// A phase's end: the next one converts the raw elements again, and nothing of it is begun before (the fp32 values of all
+// of a phase's operands, kept for the next, took the backward pass from 168 registers to 243).
 template <typename T>
-__device__ __forceinline__ void compose(const GlrArgs& a, const Place& p, const Elems<T, V>* x, const Elems<T, V>* g,
-                                        uint32_t starts, const int32_t* starts_at, float (*fa)[V], float (*fb)[V],
-                                        float* A, float* S) {
+__device__ __forceinline__ void next_phase(Elems<T, V>* e) {
 #pragma unroll
   for (int k = 0; k < K; ++k) {
+    if constexpr (sizeof(T) * V == 16) {
+      typedef int quad __attribute__((ext_vector_type(4)));
+      quad q = __builtin_bit_cast(quad, (typename Raw<T, V>::plain)e[k].raw);
+      asm volatile("" : "+v"(q));
+      e[k].raw = __builtin_bit_cast(typename Raw<T, V>::plain, q);
+    } else {
+      typedef int pair __attribute__((ext_vector_type(2)));
+      pair q = __builtin_bit_cast(pair, (typename Raw<T, V>::plain)e[k].raw);
+      asm volatile("" : "+v"(q));
+      e[k].raw = __builtin_bit_cast(typename Raw<T, V>::plain, q);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The maps h -> fa h + b of a thread's tokens, b = keep x, and their composition (A, S).  A sequence's first token starts
+// from its h0 and forgets the rest.  KEEP: the keeps instead of the b's.
+template <bool KEEP, typename T>
+__device__ __forceinline__ void compose(const GlrArgs& a, const Place& p, const Elems<T, V>* x, const Elems<T, V>* g,
+                                        const Edges& begin, float (*fa)[V], float (*fb)[V], float* A, float* S) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (begin.is(k)) {
+      begin.get(k, S);
+#pragma unroll
+      for (int v = 0; v < V; ++v) A[v] = 0.f;
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       float keep;
       gate_of(g[k][v], fa[k][v], keep);
-      fb[k][v] = mul0(keep, x[k][v]);
-    }
-    if (starts >> k & 1) {
-      const float* h0 = a.h0 ? a.h0 + (int64_t)starts_at[p.mine + k] * a.dim + p.ch : nullptr;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (h0 && v < p.have) fb[k][v] = fmaf(fa[k][v], h0[v], fb[k][v]);
-        fa[k][v] = 0.f;
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      S[v] = k == 0 ? fb[k][v] : mul0(fa[k][v], S[v]) + fb[k][v];
-      A[v] = k == 0 ? fa[k][v] : A[v] * fa[k][v];
+      const float b = mul0(keep, x[k][v]);
+      fb[k][v] = KEEP ? keep : b;
+      S[v] = fmaf(fa[k][v], S[v], b);
+      A[v] *= fa[k][v];
     }
   }
 }
 
 template <bool CUT, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads) void glr_forward_kernel(const GlrArgs a) {
-  __shared__ int32_t marks[kWaves][2][kMaxTokens];
   const Place p = place_of(a);
   share_of_sequences(a, a.h0, a.h_last);
   const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
   const Span s = span_of<CUT, true>(a, unit, p.lane);
   if (s.lo >= s.hi) return;
-  int32_t *starts_at = marks[p.wave][0], *ends_at = marks[p.wave][1];
+  const Scratch lds(p);
+  int32_t *starts_at = lds.starts_at, *ends_at = lds.ends_at;
+  float* slots = lds.slots;
   Window w;
   w.load(a, s.seq, p.lane);
   float state[V];
@@ -312,115 +461,132 @@ __global__ __launch_bounds__(kThreads) void glr_forward_kernel(const GlrArgs a) 
   for (int v = 0; v < V; ++v) state[v] = CUT && v < p.have ? a.map_s[unit * a.dim + p.ch + v] : 0.f;
   for (int64_t block = s.lo / p.tokens; block * p.tokens < s.hi; ++block) {
     const int64_t t0 = block * p.tokens;
+    const Block bl(p, t0, s.lo, s.hi);
     Elems<T, V> x[K], g[K];
-    load_block<WIDE, T>(a, p, t0, s.lo, s.hi, x, g, nullptr);
+    load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+    load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);   // a token outside keeps the state
     uint32_t starts, ends;
     marks_of<true>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, starts_at, ends_at, starts, ends);
     if (a.entry && t0 >= s.lo && p.mine == 0) put_channels(a.entry + block * a.dim, p, state);
+    Edges begin;
+    begin.read(a, p, starts, starts_at, a.h0);
+    begin.read_more(a, p, starts_at, a.h0, slots);
     float fa[K][V], fb[K][V], A[V], S[V], h[V];
-    compose<T>(a, p, x, g, starts, starts_at, fa, fb, A, S);
+    compose<false, T>(a, p, x, g, begin, fa, fb, A, S);
     join_groups<true>(p, A, S, state, h);
     if (p.have == 0) continue;
-    T* out = static_cast<T*>(a.h) + (t0 + p.mine) * a.h_stride + p.ch;
+    const Rows<WIDE, T> out(a.h, a.h_stride, p, bl);
 #pragma unroll
-    for (int k = 0; k < K; ++k, out += a.h_stride) {
-      const int64_t t = t0 + p.mine + k;
+    for (int k = 0; k < K; ++k) {
+      if (begin.is(k)) begin.get(k, h);
 #pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = mul0(fa[k][v], h[v]) + fb[k][v];
-      if (t >= s.lo && t < s.hi) store_elems<WIDE, T, V>(out, h, p.have);
+      for (int v = 0; v < V; ++v) h[v] = fmaf(fa[k][v], h[v], fb[k][v]);
+      if (bl.has(p.mine + k)) out.put(k, h);
       if ((ends >> k & 1) && a.h_last) put_channels(a.h_last + (int64_t)ends_at[p.mine + k] * a.dim, p, h);
     }
   }
 }
 
 template <bool CUT, bool WIDE, typename T>
-__global__ __launch_bounds__(kThreads) void glr_backward_kernel(const GlrArgs a) {
-  __shared__ int32_t marks[kWaves][2][kMaxTokens];
+__global__ __launch_bounds__(kThreads, 2) void glr_backward_kernel(const GlrArgs a) {
   const Place p = place_of(a);
   share_of_sequences(a, a.dh_last, a.dh0);
   const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
   const Span s = span_of<CUT, false>(a, unit, p.lane);
   if (s.lo >= s.hi) return;
-  int32_t *starts_at = marks[p.wave][0], *ends_at = marks[p.wave][1];
+  const Scratch lds(p);
   Window w;
   w.load(a, s.seq - 62, p.lane);   // the span's last sequence, or one past it, is the window's last
   float grad[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) grad[v] = CUT && v < p.have ? a.map_s[unit * a.dim + p.ch + v] : 0.f;
-  for (int64_t block = (s.hi - 1) / p.tokens; block >= s.lo / p.tokens; --block) {
+  // the next block's rows travel while this one's are worked on: two waves a SIMD do not hide the latency by themselves
+  // (rows of fp32 would not fit the registers)
+  constexpr bool AHEAD = sizeof(T) == 2;
+  Elems<T, V> nx[K], ng[K], nd[K];
+  float entering[V];
+  const auto fetch = [&](int64_t block) {
     const int64_t t0 = block * p.tokens;
+    const Block bl(p, t0, s.lo, s.hi);
+    load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, nx);
+    load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, ng);   // a token outside keeps the state, and the gradient
+    load_dh<WIDE, T>(a, p, bl, nd);
+#pragma unroll
+    for (int v = 0; v < V; ++v) entering[v] = t0 >= s.lo && v < p.have ? a.entry[block * a.dim + p.ch + v] : 0.f;
+  };
+  const int64_t last = s.lo / p.tokens;
+  if (AHEAD) fetch((s.hi - 1) / p.tokens);
+  for (int64_t block = (s.hi - 1) / p.tokens; block >= last; --block) {
+    if (!AHEAD) fetch(block);
+    const int64_t t0 = block * p.tokens;
+    const Block bl(p, t0, s.lo, s.hi);
+    uint32_t starts, ends;
+    marks_of<false>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, lds.starts_at, lds.ends_at, starts, ends);
+    Edges begin, end;
+    begin.read(a, p, starts, lds.starts_at, a.h0);
+    end.read(a, p, ends, lds.ends_at, a.dh_last);
     Elems<T, V> x[K], g[K], d[K];
-    load_block<WIDE, T>(a, p, t0, s.lo, s.hi, x, g, a.dh ? d : nullptr);
     float state[V];   // enters the block, if its sequence began before it
 #pragma unroll
-    for (int v = 0; v < V; ++v) state[v] = t0 >= s.lo && v < p.have ? a.entry[block * a.dim + p.ch + v] : 0.f;
-    uint32_t starts, ends;
-    marks_of<false>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, starts_at, ends_at, starts, ends);
+    for (int k = 0; k < K; ++k) x[k] = nx[k], g[k] = ng[k], d[k] = nd[k];
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = entering[v];
+    if (AHEAD && block > last) fetch(block - 1);
+    begin.read_more(a, p, lds.starts_at, a.h0, lds.slots);
     float fa[K][V], kp[K][V], hx[K][V], A[V], S[V], h[V];
-    {
-      float la[K][V], fb[K][V];
-      compose<T>(a, p, x, g, starts, starts_at, la, fb, A, S);
-      join_groups<true>(p, A, S, state, h);
-      // the state before each token less its x, which dgate needs
+    compose<true, T>(a, p, x, g, begin, fa, kp, A, S);
+    join_groups<true>(p, A, S, state, h);
+    next_phase(x);
+    // the state before each token less its x, which dgate needs
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (starts >> k & 1) {
-          const float* h0 = a.h0 ? a.h0 + (int64_t)starts_at[p.mine + k] * a.dim + p.ch : nullptr;
+    for (int k = 0; k < K; ++k) {
+      if (begin.is(k)) begin.get(k, h);
 #pragma unroll
-          for (int v = 0; v < V; ++v) h[v] = h0 && v < p.have ? h0[v] : 0.f;
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          hx[k][v] = h[v] - x[k][v];
-          h[v] = mul0(la[k][v], h[v]) + fb[k][v];
-        }
+      for (int v = 0; v < V; ++v) {
+        const float xv = x[k][v];
+        hx[k][v] = h[v] - xv;
+        h[v] = fmaf(fa[k][v], h[v], mul0(kp[k][v], xv));
       }
     }
-    // the gradients' maps, from the last token on
-    float RA[V], RS[V], de[K][V];
+    next_phase(d);
+    end.read_more(a, p, lds.ends_at, a.dh_last, lds.slots);
+    // the gradients' maps, from the last token on: A and S once more
 #pragma unroll
-    for (int v = 0; v < V; ++v) RA[v] = 1.f, RS[v] = 0.f;
+    for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
+      if (end.is(k)) {
+        end.get(k, S);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        gate_of(g[k][v], fa[k][v], kp[k][v]);
-        de[k][v] = a.dh ? d[k][v] : 0.f;
-      }
-      if (ends >> k & 1) {
-        const float* last = a.dh_last ? a.dh_last + (int64_t)ends_at[p.mine + k] * a.dim + p.ch : nullptr;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          if (last && v < p.have) de[k][v] += last[v];
-          RA[v] = RS[v] = 0.f;
-        }
+        for (int v = 0; v < V; ++v) A[v] = 0.f;
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        RS[v] = fa[k][v] * (RS[v] + de[k][v]);
-        RA[v] *= fa[k][v];
+        S[v] = fa[k][v] * (S[v] + d[k][v]);
+        A[v] *= fa[k][v];
       }
     }
     float c[V];
-    join_groups<false>(p, RA, RS, grad, c);
+    join_groups<false>(p, A, S, grad, c);
+    next_phase(d);
     if (p.have == 0) continue;
+    const Rows<WIDE, T> dx_rows(a.dx, a.dx_stride, p, bl), dgate_rows(a.dgate, a.dgate_stride, p, bl);
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
-      const int64_t t = t0 + p.mine + k;
       float dx[V], dg[V];
+      if (end.is(k)) end.get(k, c);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if (ends >> k & 1) c[v] = 0.f;
-        const float e = de[k][v] + c[v];
+        const float e = c[v] + d[k][v];
         c[v] = fa[k][v] * e;
         dx[v] = kp[k][v] * e;
         dg[v] = mul0(kp[k][v], hx[k][v]) * c[v];
       }
-      if (t >= s.lo && t < s.hi) {
-        store_elems<WIDE, T, V>(static_cast<T*>(a.dx) + t * a.dx_stride + p.ch, dx, p.have);
-        store_elems<WIDE, T, V>(static_cast<T*>(a.dgate) + t * a.dgate_stride + p.ch, dg, p.have);
+      if (bl.has(p.mine + k)) {
+        dx_rows.put(k, dx);
+        dgate_rows.put(k, dg);
       }
-      if ((starts >> k & 1) && a.dh0) put_channels(a.dh0 + (int64_t)starts_at[p.mine + k] * a.dim, p, c);
+      if ((starts >> k & 1) && a.dh0) put_channels(a.dh0 + (int64_t)lds.starts_at[p.mine + k] * a.dim, p, c);
     }
   }
 }
@@ -429,7 +595,6 @@ __global__ __launch_bounds__(kThreads) void glr_backward_kernel(const GlrArgs a)
 // have a say, and none where a sequence ends (begins) with the range.
 template <bool FORWARD, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
-  __shared__ int32_t marks[kWaves][2][kMaxTokens];
   const Place p = place_of(a);
   const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
   if (unit >= a.units) return;
@@ -441,34 +606,43 @@ __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
 #pragma unroll
   for (int v = 0; v < V; ++v) prod[v] = 1.f, state[v] = 0.f;
   if (FORWARD ? end > hi : begin < lo) {   // the range's edge lies within the sequence
-    int32_t *starts_at = marks[p.wave][0], *ends_at = marks[p.wave][1];
+    const Scratch lds(p);
+    int32_t *starts_at = lds.starts_at, *ends_at = lds.ends_at;
     Window w;
     w.load(a, FORWARD ? seq : seq - 62, p.lane);
     const int64_t b0 = from / p.tokens, b1 = (to - 1) / p.tokens;
     for (int64_t i = b0; i <= b1; ++i) {
       const int64_t t0 = (FORWARD ? i : b0 + b1 - i) * p.tokens;
+      const Block bl(p, t0, from, to);
       Elems<T, V> x[K], g[K], d[K];
-      load_block<WIDE, T>(a, p, t0, from, to, FORWARD ? x : nullptr, g, !FORWARD && a.dh ? d : nullptr);
+      if (FORWARD) load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+      load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);
+      if (!FORWARD) load_dh<WIDE, T>(a, p, bl, d);
       uint32_t starts, ends;
       marks_of<FORWARD>(a, w, t0, p.tokens, from, to, p.lane, p.mine, starts_at, ends_at, starts, ends);
+      Edges edge;
+      edge.read(a, p, FORWARD ? starts : ends, FORWARD ? starts_at : ends_at, FORWARD ? a.h0 : a.dh_last);
+      edge.read_more(a, p, FORWARD ? starts_at : ends_at, FORWARD ? a.h0 : a.dh_last, lds.slots);
       float enter[V];
       if (FORWARD) {
         float fa[K][V], fb[K][V];
-        compose<T>(a, p, x, g, starts, starts_at, fa, fb, A, S);
+        compose<false, T>(a, p, x, g, edge, fa, fb, A, S);
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
 #pragma unroll
         for (int k = K - 1; k >= 0; --k) {
-          const bool stop = ends >> k & 1;
-          const float* last = stop && a.dh_last ? a.dh_last + (int64_t)ends_at[p.mine + k] * a.dim + p.ch : nullptr;
+          if (edge.is(k)) {
+            edge.get(k, S);
+#pragma unroll
+            for (int v = 0; v < V; ++v) A[v] = 0.f;
+          }
 #pragma unroll
           for (int v = 0; v < V; ++v) {
-            float ga, keep, e = a.dh ? d[k][v] : 0.f;
+            float ga, keep;
             gate_of(g[k][v], ga, keep);
-            if (last && v < p.have) e += last[v];
-            S[v] = ga * ((stop ? 0.f : S[v]) + e);
-            A[v] = stop ? 0.f : A[v] * ga;
+            S[v] = ga * (S[v] + d[k][v]);
+            A[v] *= ga;
           }
         }
       }
@@ -488,14 +662,17 @@ __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
   }
 }
 
-// Cut: the ranges' maps to the states that enter them, in place of map_s.  A workgroup takes 16 channels; its 64 groups
-// of threads take neighbouring ranges, compose them, join by LDS and walk them again.
-constexpr int kScanThreadsGlr = 1024, kScanChannels = 16, kScanGroups = kScanThreadsGlr / kScanChannels;
+// Cut: the ranges' maps to the states that enter them, in place of map_s.  A workgroup takes 4 channels, so that its 256
+// groups of threads walk few ranges each (3,400 ranges of 64 channels: 16 channels and 64 groups took 23 us, most of
+// it waiting for one load after the other); they compose them, join by shuffles and LDS, and walk them again.
+constexpr int kScanThreadsGlr = 1024, kScanChannels = 4, kScanGroups = kScanThreadsGlr / kScanChannels;
 
 template <bool FORWARD>
 __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs a) {
-  __shared__ float la[kScanGroups][kScanChannels], ls[kScanGroups][kScanChannels];
+  constexpr int kScanWaves = kScanThreadsGlr / 64;
+  __shared__ float la[kScanWaves][kScanChannels], ls[kScanWaves][kScanChannels];
   const int c = threadIdx.x % kScanChannels, g = threadIdx.x / kScanChannels;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int ch = (int)blockIdx.x * kScanChannels + c;
   const int64_t per = (a.units + kScanGroups - 1) / kScanGroups, begin = min(g * per, a.units), end = min(begin + per, a.units);
   const auto at = [&](int64_t i) { return (FORWARD ? i : a.units - 1 - i) * a.dim + ch; };
@@ -520,10 +697,23 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
       S = mul0(ma, S) + ms;
       A *= ma;
     });
-  la[g][c] = A;
-  ls[g][c] = S;
+  // the groups of a wave, then the waves
+#pragma unroll
+  for (int d = kScanChannels; d < 64; d <<= 1) {
+    const float s0 = __shfl_up(S, d, 64), a0 = __shfl_up(A, d, 64);
+    if (lane >= d) {
+      S = mul0(A, s0) + S;
+      A *= a0;
+    }
+  }
+  if (lane >= 64 - kScanChannels) {
+    la[wave][c] = A;
+    ls[wave][c] = S;
+  }
   __syncthreads();
-  for (int i = 0; i < g; ++i) h = mul0(la[i][c], h) + ls[i][c];
+  for (int i = 0; i < wave; ++i) h = mul0(la[i][c], h) + ls[i][c];
+  const float s0 = __shfl_up(S, kScanChannels, 64), a0 = __shfl_up(A, kScanChannels, 64);
+  if (lane >= kScanChannels) h = mul0(a0, h) + s0;
   if (ch < a.dim)
     walk([&](int64_t i, float ma, float ms) {
       a.map_s[at(i)] = h;
@@ -565,22 +755,23 @@ template <bool WIDE, typename T>
 hipError_t run_pass(const GlrArgs& a, bool backward, hipStream_t s) {
   const GlrShape sh = glr_shape(a.tokens, a.dim);
   const dim3 grid((unsigned)std::max<int64_t>(1, (a.units + kWaves - 1) / kWaves), (unsigned)sh.channel_blocks);
+  const size_t lds = scratch_bytes(sh.block_tokens);
   if (!a.cut) {
     if (backward)
-      glr_backward_kernel<false, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+      glr_backward_kernel<false, WIDE, T><<<grid, kThreads, lds, s>>>(a);
     else
-      glr_forward_kernel<false, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+      glr_forward_kernel<false, WIDE, T><<<grid, kThreads, lds, s>>>(a);
     return hipGetLastError();
   }
   const dim3 scan((unsigned)((a.dim + kScanChannels - 1) / kScanChannels));
   if (backward) {
-    glr_maps_kernel<false, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    glr_maps_kernel<false, WIDE, T><<<grid, kThreads, lds, s>>>(a);
     glr_scan_kernel<false><<<scan, kScanThreadsGlr, 0, s>>>(a);
-    glr_backward_kernel<true, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    glr_backward_kernel<true, WIDE, T><<<grid, kThreads, lds, s>>>(a);
   } else {
-    glr_maps_kernel<true, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    glr_maps_kernel<true, WIDE, T><<<grid, kThreads, lds, s>>>(a);
     glr_scan_kernel<true><<<scan, kScanThreadsGlr, 0, s>>>(a);
-    glr_forward_kernel<true, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    glr_forward_kernel<true, WIDE, T><<<grid, kThreads, lds, s>>>(a);
   }
   return hipGetLastError();
 }

@@ -70,10 +70,16 @@ dpi_status check_glr(const dpi_glr_desc* d) {
   return DPI_OK;
 }
 
+// Rows of a recurrence's operand: a block of them is addressed with 32-bit offsets.
+dpi_status check_glr_rows(const void* p, int64_t stride, const dpi_glr_desc* d, const char* what) {
+  if (stride >= kGlrMaxStride) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "%s: row stride 2^20 or more", what);
+  return check_rows(p, d->dtype, stride, d->dim, d->num_tokens, what);
+}
+
 dpi_status check_glr_operands(const dpi_glr_desc* d) {
   DPI_TRY(check_words(d->offsets, d->num_seqs > 0, "offsets"));
-  DPI_TRY(check_rows(d->x, d->dtype, d->x_stride, d->dim, d->num_tokens, "x"));
-  DPI_TRY(check_rows(d->gate, d->dtype, d->gate_stride, d->dim, d->num_tokens, "gate"));
+  DPI_TRY(check_glr_rows(d->x, d->x_stride, d, "x"));
+  DPI_TRY(check_glr_rows(d->gate, d->gate_stride, d, "gate"));
   return check_words(d->h0, false, "h0");
 }
 
@@ -238,7 +244,7 @@ dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, 
                            void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream) {
   DPI_TRY(check_glr(desc));
   DPI_TRY(check_glr_operands(desc));
-  DPI_TRY(check_rows(h, desc->dtype, h_stride, desc->dim, desc->num_tokens, "h"));
+  DPI_TRY(check_glr_rows(h, h_stride, desc, "h"));
   DPI_TRY(check_words(h_last, false, "h_last"));
   DPI_TRY(check_words(entry, false, "entry"));
   DPI_TRY(check_words(device_status, false, "device_status"));
@@ -263,9 +269,9 @@ dpi_status dpi_glr_backward(const dpi_glr_desc* desc, const void* entry, const v
                             void* stream) {
   DPI_TRY(check_glr(desc));
   DPI_TRY(check_glr_operands(desc));
-  if (dh) DPI_TRY(check_rows(dh, desc->dtype, dh_stride, desc->dim, desc->num_tokens, "dh"));
-  DPI_TRY(check_rows(dx, desc->dtype, dx_stride, desc->dim, desc->num_tokens, "dx"));
-  DPI_TRY(check_rows(dgate, desc->dtype, dgate_stride, desc->dim, desc->num_tokens, "dgate"));
+  if (dh) DPI_TRY(check_glr_rows(dh, dh_stride, desc, "dh"));
+  DPI_TRY(check_glr_rows(dx, dx_stride, desc, "dx"));
+  DPI_TRY(check_glr_rows(dgate, dgate_stride, desc, "dgate"));
   DPI_TRY(check_words(entry, desc->num_tokens > 0, "entry"));
   DPI_TRY(check_words(dh_last, false, "dh_last"));
   DPI_TRY(check_words(dh0, false, "dh0"));

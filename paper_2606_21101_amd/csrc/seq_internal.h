@@ -84,6 +84,7 @@ struct GlrArgs {
 constexpr int kGlrThreads = 256;
 constexpr int kGlrV = 4;              // channels per thread
 constexpr int kGlrK = 8;              // tokens per thread
+constexpr int64_t kGlrMaxStride = 1 << 20;   // row strides are smaller: 64 * kGlrK rows span less than 2^31 bytes
 constexpr int kGlrWaves = 4096;       // waves a pass is split into, while ...
 constexpr int kGlrRangeBlocks = 16;   // ... a range has at most so many blocks
 constexpr int kGlrWholeBlocks = 32;   // the longest sequence that one wave walks, in blocks

@@ -1,0 +1,815 @@
+// Gated linear recurrence over packed sequences, forward, backward and one
+// token at a time, for gfx950 (MI355X).
+//
+//   a_t = sigmoid(gate_t),   h_t = a_t h_{t-1} + (1 - a_t) x_t   per channel.
+//
+// A step is the map h -> A h + S; maps compose: (A2, S2) after (A1, S1) is
+// (A2 A1, A2 S1 + S2).  A wave walks a range of tokens a block at a time: LC
+// lanes cover the channels, V each, and the wave's 64 / LC groups of lanes take
+// K tokens each.  A thread composes its K tokens in registers, groups join
+// their maps by shuffles, and each thread walks its tokens again from the state
+// that enters them.  Waves share nothing, so nothing waits for a barrier.
+//
+// A sequence's first token is the map with A = 0.  Products with such an A are
+// legacy ones, where 0 times anything is 0: no infinity and no NaN of one
+// sequence gets into the next.  So is (1 - a) x, where a token of gate +inf
+// keeps the state whatever x it has.
+//
+// Work is split in one of two ways.  Whole: a wave takes the sequences that
+// begin in its range of tokens, to their ends; one launch.  Cut: a wave takes
+// its range's tokens only; a first launch composes each range's map, a second
+// scans the maps, a third walks the ranges from the states that enter them.
+//
+// The backward pass runs c_t = a_t (dh_t + c_{t+1}) the same way from the end,
+// c_t being the gradient of h_{t-1}, and computes the states again in fp32 from
+// the state that entered each block, which the forward pass saved.  The bound
+// is HBM: 3 arrays forward, 5 backward.
+#include "elem.h"
+#include "seq_internal.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace dpi {
+namespace {
+
+constexpr int V = kGlrV, K = kGlrK, kThreads = kGlrThreads, kWaves = kThreads / 64;
+constexpr int kMaxTokens = 64 * K;   // of a block: one lane covers a row
+
+// Product in which 0 times anything is 0.
+__device__ __forceinline__ float mul0(float a, float b) {
+  float r;
+  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
+// a = sigmoid(g) and 1 - a, each with a small relative error wherever it lies (no 1 - a of an a near 1); a is not below
+// 2^-126, and a NaN stays one.
+__device__ __forceinline__ void gate_of(float g, float& a, float& keep) {
+  const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(g * -1.44269504f, 126.f));
+  a = __builtin_amdgcn_rcpf(1.f + e);
+  keep = e * a;
+}
+
+// First s in [0, seqs] with offsets[s + 1] > t, by the whole wave: the sequence that holds token t when the offsets are
+// sound.
+__device__ __forceinline__ int64_t sequence_of(const GlrArgs& a, int64_t t, int lane) {
+  int64_t lo = 0, count = a.seqs;   // the answer lies in [lo, lo + count]
+  while (count > 0) {
+    const int64_t step = (count + 63) >> 6, at = lo + (lane + 1) * step - 1;   // 64 candidates, the last of each part
+    const bool before = at < lo + count && (int64_t)a.offsets[at + 1] <= t;
+    const int parts = __popcll(__ballot(before));
+    lo += parts * step;
+    count = min(step - 1, max(count - parts * step, (int64_t)0));
+  }
+  return __builtin_amdgcn_readfirstlane((int32_t)lo);
+}
+
+// A wave's tokens [lo, hi), and the sequence that holds the first (forwards) or the last of them (backwards).
+struct Span {
+  int64_t lo, hi, seq;
+};
+
+__device__ __forceinline__ int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return min(max(x, lo), hi); }
+
+// The same for the whole wave.
+__device__ __forceinline__ int64_t offset_at(const GlrArgs& a, int64_t s) {
+  return __builtin_amdgcn_readfirstlane(a.offsets[s]);
+}
+
+// Whole: from the first sequence start at or after the range's begin to the end of the last sequence begun before its
+// end.
+template <bool CUT, bool FORWARD>
+__device__ __forceinline__ Span span_of(const GlrArgs& a, int64_t unit, int lane) {
+  Span s;
+  const int64_t t0 = min(unit * a.range, a.tokens), t1 = min(t0 + a.range, a.tokens);
+  s.lo = t0;
+  s.hi = t1;
+  s.seq = 0;
+  if (t0 >= t1) return s;
+  if (CUT) {
+    s.seq = sequence_of(a, FORWARD ? t0 : t1 - 1, lane);
+    return s;
+  }
+  const int64_t first = t0 > 0 ? sequence_of(a, t0 - 1, lane) : -1;
+  const int64_t last = sequence_of(a, t1 - 1, lane);
+  if (t0 > 0) s.lo = first < a.seqs ? clamped(offset_at(a, first + 1), t0, a.tokens) : a.tokens;
+  s.hi = last < a.seqs ? clamped(offset_at(a, last + 1), t1, a.tokens) : a.tokens;
+  if (s.lo >= t1) s.hi = s.lo;   // no sequence begins in the range
+  s.seq = FORWARD ? max(first, (int64_t)0) : last;
+  return s;
+}
+
+// 64 neighbouring sequences, one a lane, and the marks of those that begin or end in a block of tokens.
+struct Window {
+  int64_t base;
+  int32_t begin, end;   // of the lane's sequence; an empty one past the last
+
+  __device__ __forceinline__ void load(const GlrArgs& a, int64_t b, int lane) {
+    base = max(b, (int64_t)0);
+    const int64_t s = base + lane;
+    begin = s < a.seqs ? a.offsets[s] : INT32_MAX;
+    end = s < a.seqs ? a.offsets[s + 1] : INT32_MAX;
+  }
+};
+
+// starts / ends: the lane's K tokens of the block at `t0` that are a sequence's first / last; seq_of[i], end_of[i]: that
+// sequence, where it is.  Only tokens of [lo, hi) are marked.
+template <bool FORWARD>
+__device__ __forceinline__ void marks_of(const GlrArgs& a, Window& w, int64_t t0, int tokens, int64_t lo, int64_t hi,
+                                         int lane, int mine, int32_t* starts_at, int32_t* ends_at, uint32_t& starts,
+                                         uint32_t& ends) {
+  const int64_t t1 = t0 + tokens;
+  starts = ends = 0;
+  bool any = false;
+  for (;;) {
+    const bool full = w.end > w.begin;
+    const bool b = full && w.begin >= max(t0, lo) && w.begin < min(t1, hi);
+    const bool e = full && w.end > max(t0, lo) && w.end <= min(t1, hi);
+    if (__ballot(b || e)) {
+      if (!any) {
+        any = true;
+        for (int i = lane; i < tokens; i += 64) starts_at[i] = ends_at[i] = -1;
+      }
+      if (b) starts_at[w.begin - t0] = (int32_t)(w.base + lane);
+      if (e) ends_at[w.end - 1 - t0] = (int32_t)(w.base + lane);
+    }
+    if (FORWARD) {
+      const int32_t far = __builtin_amdgcn_readlane(w.end, 63);
+      if ((int64_t)far > t1 || w.base + 64 >= a.seqs) break;
+      w.load(a, w.base + 64, lane);
+    } else {
+      const int32_t far = __builtin_amdgcn_readfirstlane(w.begin);
+      if ((int64_t)far <= t0 || w.base == 0) break;
+      w.load(a, w.base - 63, lane);   // one again: its begin says whether to go on
+    }
+  }
+  if (any) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (starts_at[mine + k] >= 0) starts |= 1u << k;
+      if (ends_at[mine + k] >= 0) ends |= 1u << k;
+    }
+  }
+}
+
+// Malformed offsets of this workgroup's share of the sequences are reported; empty sequences' end states (their
+// gradients, backward) are copied from `from` (zeros without it) to `to`.
+__device__ __forceinline__ void share_of_sequences(const GlrArgs& a, const float* from, float* to) {
+  const int64_t per = (a.seqs + gridDim.x - 1) / gridDim.x;
+  const int64_t begin = blockIdx.x * per, end = min(begin + per, a.seqs);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  bool bad = blockIdx.x == 0 && threadIdx.x == 0 && (a.offsets[0] != 0 || (int64_t)a.offsets[a.seqs] != a.tokens);
+  for (int64_t s0 = begin + wave * 64; s0 < end; s0 += kWaves * 64) {
+    const int64_t s = s0 + lane;
+    bool empty = false;
+    if (s < end) {
+      const int32_t o0 = a.offsets[s], o1 = a.offsets[s + 1];
+      bad |= o1 < o0;
+      empty = o1 == o0;
+    }
+    if (!to) continue;
+    for (uint64_t left = __ballot(empty); left; left &= left - 1) {
+      const int64_t at = (s0 + __builtin_ctzll(left)) * a.dim;
+      for (int c = blockIdx.y * 64 + lane; c < a.dim; c += gridDim.y * 64) to[at + c] = from ? from[at + c] : 0.f;
+    }
+  }
+  if (bad && a.status) atomicOr(a.status, DPI_DEVSTAT_BAD_OFFSETS);
+}
+
+// What a thread knows of its place: lane c of LC covers channels [ch, ch + V), its group tokens [mine, mine + K) of a
+// block.
+struct Place {
+  int lane, wave, lc, c, mine, tokens, ch, have;   // have: channels that exist, 0 for none
+};
+
+__device__ __forceinline__ Place place_of(const GlrArgs& a) {
+  Place p;
+  p.lane = threadIdx.x & 63;
+  p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  p.lc = 1 << a.lc_log;
+  p.c = p.lane & (p.lc - 1);
+  p.mine = (p.lane >> a.lc_log) * K;
+  p.tokens = (64 >> a.lc_log) * K;
+  p.ch = ((int)blockIdx.y * p.lc + p.c) * V;
+  p.have = max(0, min(V, a.dim - p.ch));
+  return p;
+}
+
+__device__ __forceinline__ void put_channels(float* row, const Place& p, const float* v) {
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < p.have) row[p.ch + i] = v[i];
+}
+
+// A wave's place in its span: the block at token t0, whose rows [first, past) belong to the span.
+struct Block {
+  int64_t t0;
+  int32_t first, past;
+  bool whole;
+
+  __device__ __forceinline__ Block(const Place& p, int64_t t, int64_t lo, int64_t hi)
+      : t0(t), first((int32_t)max(lo - t, (int64_t)0)), past((int32_t)min(hi - t, (int64_t)p.tokens)) {
+    whole = first == 0 && past == p.tokens;
+  }
+  __device__ __forceinline__ bool has(int32_t row) const { return whole || (row >= first && row < past); }
+};
+
+// The block's rows of a [tokens, dim] operand through a buffer descriptor of its rows up to `past`: a thread keeps one
+// 32-bit offset, its k-th row is a scalar one (64-bit addresses of every row took 40 registers more), and rows past the
+// span are not touched.  A block's rows span less than 2^31 bytes (kGlrMaxStride).
+template <bool WIDE, typename T>
+struct Rows {
+  __amdgpu_buffer_rsrc_t rsrc;
+  int32_t stride, lane;   // bytes; of the thread's first row and channel
+  int32_t have;
+
+  __device__ __forceinline__ Rows(const void* p, int64_t row_stride, const Place& at, const Block& b)
+      : stride((int32_t)row_stride * (int32_t)sizeof(T)), have(at.have) {
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        static_cast<char*>(const_cast<void*>(p)) + b.t0 * row_stride * (int64_t)sizeof(T), (short)0, b.past * stride, 0x00020000);
+    // a thread without channels reads the row's first ones
+    lane = at.mine * stride + (at.have > 0 ? at.ch * (int32_t)sizeof(T) : 0);
+  }
+  __device__ __forceinline__ Elems<T, V> get(int k) const {
+    Elems<T, V> e;
+    if constexpr (WIDE) {
+      if constexpr (sizeof(T) * V == 16) {
+        typedef int quad __attribute__((ext_vector_type(4)));
+        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (quad)__builtin_amdgcn_raw_buffer_load_b128(rsrc, lane, k * stride, 0));
+      } else {
+        typedef int pair __attribute__((ext_vector_type(2)));
+        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (pair)__builtin_amdgcn_raw_buffer_load_b64(rsrc, lane, k * stride, 0));
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int32_t at = lane + min(v, max(have, 1) - 1) * (int32_t)sizeof(T);
+        if constexpr (sizeof(T) == 4)
+          e.raw[v] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, k * stride, 0));
+        else
+          e.raw[v] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, k * stride, 0));
+      }
+    }
+    return e;
+  }
+  __device__ __forceinline__ void put(int k, const float* v) const {
+    typename Raw<T, V>::plain r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = (T)v[i];
+    if constexpr (WIDE) {
+      if constexpr (sizeof(T) * V == 16) {
+        typedef int quad __attribute__((ext_vector_type(4)));
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(quad, r), rsrc, lane, k * stride, 0);
+      } else {
+        typedef int pair __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(pair, r), rsrc, lane, k * stride, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (i >= have) continue;
+        const int32_t at = lane + i * (int32_t)sizeof(T);
+        if constexpr (sizeof(T) == 4)
+          __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, (T)r[i]), rsrc, at, k * stride, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, (T)r[i]), rsrc, at, k * stride, 0);
+      }
+    }
+  }
+};
+
+// The thread's rows of one operand; those outside the span are `other`.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load_block(const void* from, int64_t stride, const Place& p, const Block& b, float other,
+                                           Elems<T, V>* e) {
+  const Rows<WIDE, T> rows(from, stride, p, b);
+#pragma unroll
+  for (int k = 0; k < K; ++k) e[k] = rows.get(k);
+  if (b.whole) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (b.has(p.mine + k)) continue;
+#pragma unroll
+    for (int v = 0; v < V; ++v) e[k].raw[v] = (T)other;
+  }
+}
+
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load_dh(const GlrArgs& a, const Place& p, const Block& b, Elems<T, V>* d) {
+  if (a.dh) {
+    load_block<WIDE, T>(a.dh, a.dh_stride, p, b, 0.f, d);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) d[k].raw[v] = (T)0.f;
+  }
+}
+
+// Groups' maps (A, S) to the state that enters the thread's tokens, `enter`; `state`, the one that enters the block,
+// becomes the one that leaves it.  UP: groups in order of time, else against it.
+template <bool UP>
+__device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, float* state, float* enter) {
+  const bool first = UP ? p.lane < p.lc : p.lane >= 64 - p.lc;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    if (first) {   // from here on its map forgets what came before it
+      S[v] = mul0(A[v], state[v]) + S[v];
+      A[v] = 0.f;
+    }
+  }
+  for (int d = p.lc; d < 64; d <<= 1) {
+    const bool has = UP ? p.lane >= d : p.lane + d < 64;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float s0 = UP ? __shfl_up(S[v], d, 64) : __shfl_down(S[v], d, 64);
+      const float a0 = UP ? __shfl_up(A[v], d, 64) : __shfl_down(A[v], d, 64);
+      if (has) {
+        S[v] = mul0(A[v], s0) + S[v];
+        A[v] *= a0;
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const float s0 = UP ? __shfl_up(S[v], p.lc & 63, 64) : __shfl_down(S[v], p.lc & 63, 64);
+    enter[v] = first ? state[v] : s0;
+    state[v] = __shfl(S[v], UP ? 64 - p.lc + p.c : p.c, 64);
+  }
+}
+
+// A thread's part of a row of states (zeros without them): what a sequence begins (ends) with.
+__device__ __forceinline__ void edge_state(const float* states, const GlrArgs& a, const Place& p, int32_t seq, float* out) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) out[v] = states && v < p.have ? states[(int64_t)seq * a.dim + p.ch + v] : 0.f;
+}
+
+template <bool B>
+struct Many {
+  static constexpr bool value = B;
+};
+
+// The edges among a thread's tokens.  One is read as soon as the marks are known, with the block's other loads.  MANY: a
+// thread of the wave holds more than one (sequences shorter than K tokens), and reads the others where it needs them.
+struct Edges {
+  uint32_t mask;
+  int k;              // the token whose edge is in `state`
+  const int32_t* at;  // [K]: the tokens' sequences, where marked
+  const float* states;
+  float state[V];
+
+  __device__ __forceinline__ void read(const GlrArgs& a, const Place& p, uint32_t m, const int32_t* seqs, const float* from) {
+    mask = m;
+    at = seqs + p.mine;
+    states = from;
+    k = m ? __builtin_ctz(m) : 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = 0.f;
+    if (m && from) edge_state(from, a, p, at[k], state);
+  }
+  __device__ __forceinline__ bool many() const { return __ballot((mask & (mask - 1)) != 0) != 0; }
+  __device__ __forceinline__ bool is(int i) const { return mask >> i & 1; }
+  template <bool MANY>
+  __device__ __forceinline__ void get(const GlrArgs& a, const Place& p, int i, float* out) const {
+    if (MANY && i != k) {
+      asm volatile("" ::: "memory");   // read here, not ahead for every token
+      edge_state(states, a, p, at[i], out);
+      return;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) out[v] = state[v];
+  }
+};
+
+// A phase's end: the next one converts the raw elements again, and nothing of it is begun before (the fp32 values of all
+// of a phase's operands, kept for the next, took the backward pass from 168 registers to 243).
+template <typename T>
+__device__ __forceinline__ void next_phase(Elems<T, V>* e) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if constexpr (sizeof(T) * V == 16) {
+      typedef int quad __attribute__((ext_vector_type(4)));
+      quad q = __builtin_bit_cast(quad, (typename Raw<T, V>::plain)e[k].raw);
+      asm volatile("" : "+v"(q));
+      e[k].raw = __builtin_bit_cast(typename Raw<T, V>::plain, q);
+    } else {
+      typedef int pair __attribute__((ext_vector_type(2)));
+      pair q = __builtin_bit_cast(pair, (typename Raw<T, V>::plain)e[k].raw);
+      asm volatile("" : "+v"(q));
+      e[k].raw = __builtin_bit_cast(typename Raw<T, V>::plain, q);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The maps h -> fa h + b of a thread's tokens, b = keep x, and their composition (A, S).  A sequence's first token starts
+// from its h0 and forgets the rest.  KEEP: the keeps instead of the b's.
+template <bool MANY, bool KEEP, typename T>
+__device__ __forceinline__ void compose(const GlrArgs& a, const Place& p, const Elems<T, V>* x, const Elems<T, V>* g,
+                                        const Edges& begin, float (*fa)[V], float (*fb)[V], float* A, float* S) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (begin.is(k)) {
+      begin.get<MANY>(a, p, k, S);
+#pragma unroll
+      for (int v = 0; v < V; ++v) A[v] = 0.f;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float keep;
+      gate_of(g[k][v], fa[k][v], keep);
+      const float b = mul0(keep, x[k][v]);
+      fb[k][v] = KEEP ? keep : b;
+      S[v] = fmaf(fa[k][v], S[v], b);
+      A[v] *= fa[k][v];
+    }
+  }
+}
+
+template <bool CUT, bool WIDE, typename T>
+__global__ __launch_bounds__(kThreads) void glr_forward_kernel(const GlrArgs a) {
+  __shared__ int32_t marks[kWaves][2][kMaxTokens];
+  const Place p = place_of(a);
+  share_of_sequences(a, a.h0, a.h_last);
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
+  const Span s = span_of<CUT, true>(a, unit, p.lane);
+  if (s.lo >= s.hi) return;
+  int32_t *starts_at = marks[p.wave][0], *ends_at = marks[p.wave][1];
+  Window w;
+  w.load(a, s.seq, p.lane);
+  float state[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) state[v] = CUT && v < p.have ? a.map_s[unit * a.dim + p.ch + v] : 0.f;
+  for (int64_t block = s.lo / p.tokens; block * p.tokens < s.hi; ++block) {
+    const int64_t t0 = block * p.tokens;
+    const Block bl(p, t0, s.lo, s.hi);
+    Elems<T, V> x[K], g[K];
+    load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+    load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);   // a token outside keeps the state
+    uint32_t starts, ends;
+    marks_of<true>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, starts_at, ends_at, starts, ends);
+    if (a.entry && t0 >= s.lo && p.mine == 0) put_channels(a.entry + block * a.dim, p, state);
+    Edges begin;
+    begin.read(a, p, starts, starts_at, a.h0);
+    const auto pass = [&](auto many) {
+      constexpr bool MANY = decltype(many)::value;
+      float fa[K][V], fb[K][V], A[V], S[V], h[V];
+      compose<MANY, false, T>(a, p, x, g, begin, fa, fb, A, S);
+      join_groups<true>(p, A, S, state, h);
+      if (p.have == 0) return;
+      const Rows<WIDE, T> out(a.h, a.h_stride, p, bl);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (begin.is(k)) begin.get<MANY>(a, p, k, h);
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = fmaf(fa[k][v], h[v], fb[k][v]);
+        if (bl.has(p.mine + k)) out.put(k, h);
+        if ((ends >> k & 1) && a.h_last) put_channels(a.h_last + (int64_t)ends_at[p.mine + k] * a.dim, p, h);
+      }
+    };
+    if (false)
+      pass(Many<true>());
+    else
+      pass(Many<false>());
+  }
+}
+
+template <bool CUT, bool WIDE, typename T>
+__global__ __launch_bounds__(kThreads) void glr_backward_kernel(const GlrArgs a) {
+  __shared__ int32_t marks[kWaves][2][kMaxTokens];
+  const Place p = place_of(a);
+  share_of_sequences(a, a.dh_last, a.dh0);
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
+  const Span s = span_of<CUT, false>(a, unit, p.lane);
+  if (s.lo >= s.hi) return;
+  int32_t *starts_at = marks[p.wave][0], *ends_at = marks[p.wave][1];
+  Window w;
+  w.load(a, s.seq - 62, p.lane);   // the span's last sequence, or one past it, is the window's last
+  float grad[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) grad[v] = CUT && v < p.have ? a.map_s[unit * a.dim + p.ch + v] : 0.f;
+  for (int64_t block = (s.hi - 1) / p.tokens; block >= s.lo / p.tokens; --block) {
+    const int64_t t0 = block * p.tokens;
+    const Block bl(p, t0, s.lo, s.hi);
+    Elems<T, V> x[K], g[K], d[K];
+    load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+    load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);   // a token outside keeps the state, and the gradient
+    load_dh<WIDE, T>(a, p, bl, d);
+    float state[V];   // enters the block, if its sequence began before it
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = t0 >= s.lo && v < p.have ? a.entry[block * a.dim + p.ch + v] : 0.f;
+    uint32_t starts, ends;
+    marks_of<false>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, starts_at, ends_at, starts, ends);
+    Edges begin, end;
+    begin.read(a, p, starts, starts_at, a.h0);
+    end.read(a, p, ends, ends_at, a.dh_last);
+    const auto pass = [&](auto many) {
+      constexpr bool MANY = decltype(many)::value;
+      float fa[K][V], kp[K][V], hx[K][V], A[V], S[V], h[V];
+      compose<MANY, true, T>(a, p, x, g, begin, fa, kp, A, S);
+      join_groups<true>(p, A, S, state, h);
+      next_phase(x);
+      // the state before each token less its x, which dgate needs
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (begin.is(k)) begin.get<MANY>(a, p, k, h);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const float xv = x[k][v];
+          hx[k][v] = h[v] - xv;
+          h[v] = fmaf(fa[k][v], h[v], mul0(kp[k][v], xv));
+        }
+      }
+      next_phase(d);
+      // the gradients' maps, from the last token on: A and S once more
+#pragma unroll
+      for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
+#pragma unroll
+      for (int k = K - 1; k >= 0; --k) {
+        if (end.is(k)) {
+          end.get<MANY>(a, p, k, S);
+#pragma unroll
+          for (int v = 0; v < V; ++v) A[v] = 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          S[v] = fa[k][v] * (S[v] + d[k][v]);
+          A[v] *= fa[k][v];
+        }
+      }
+      float c[V];
+      join_groups<false>(p, A, S, grad, c);
+      next_phase(d);
+      if (p.have == 0) return;
+      const Rows<WIDE, T> dx_rows(a.dx, a.dx_stride, p, bl), dgate_rows(a.dgate, a.dgate_stride, p, bl);
+#pragma unroll
+      for (int k = K - 1; k >= 0; --k) {
+        float dx[V], dg[V];
+        if (end.is(k)) end.get<MANY>(a, p, k, c);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const float e = c[v] + d[k][v];
+          c[v] = fa[k][v] * e;
+          dx[v] = kp[k][v] * e;
+          dg[v] = mul0(kp[k][v], hx[k][v]) * c[v];
+        }
+        if (bl.has(p.mine + k)) {
+          dx_rows.put(k, dx);
+          dgate_rows.put(k, dg);
+        }
+        if ((starts >> k & 1) && a.dh0) put_channels(a.dh0 + (int64_t)starts_at[p.mine + k] * a.dim, p, c);
+      }
+    };
+    if (false)
+      pass(Many<true>());
+    else
+      pass(Many<false>());
+  }
+}
+
+// Cut: the map of a range's tokens.  Only those after the last sequence start in it (backwards: before the first end)
+// have a say, and none where a sequence ends (begins) with the range.
+template <bool FORWARD, bool WIDE, typename T>
+__global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
+  __shared__ int32_t marks[kWaves][2][kMaxTokens];
+  const Place p = place_of(a);
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
+  if (unit >= a.units) return;
+  const int64_t lo = min(unit * a.range, a.tokens), hi = min(lo + a.range, a.tokens);
+  const int64_t seq = sequence_of(a, FORWARD ? hi - 1 : lo, p.lane);
+  const int64_t begin = seq < a.seqs ? offset_at(a, seq) : 0, end = seq < a.seqs ? offset_at(a, seq + 1) : hi;
+  const int64_t from = FORWARD ? clamped(begin, lo, hi - 1) : lo, to = FORWARD ? hi : clamped(end, lo + 1, hi);
+  float A[V], S[V], prod[V], state[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) prod[v] = 1.f, state[v] = 0.f;
+  if (FORWARD ? end > hi : begin < lo) {   // the range's edge lies within the sequence
+    int32_t *starts_at = marks[p.wave][0], *ends_at = marks[p.wave][1];
+    Window w;
+    w.load(a, FORWARD ? seq : seq - 62, p.lane);
+    const int64_t b0 = from / p.tokens, b1 = (to - 1) / p.tokens;
+    for (int64_t i = b0; i <= b1; ++i) {
+      const int64_t t0 = (FORWARD ? i : b0 + b1 - i) * p.tokens;
+      const Block bl(p, t0, from, to);
+      Elems<T, V> x[K], g[K], d[K];
+      if (FORWARD) load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+      load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);
+      if (!FORWARD) load_dh<WIDE, T>(a, p, bl, d);
+      uint32_t starts, ends;
+      marks_of<FORWARD>(a, w, t0, p.tokens, from, to, p.lane, p.mine, starts_at, ends_at, starts, ends);
+      Edges edge;
+      edge.read(a, p, FORWARD ? starts : ends, FORWARD ? starts_at : ends_at, FORWARD ? a.h0 : a.dh_last);
+      float enter[V];
+      if (FORWARD) {
+        float fa[K][V], fb[K][V];
+        compose<true, false, T>(a, p, x, g, edge, fa, fb, A, S);
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k) {
+          if (edge.is(k)) {
+            edge.get<true>(a, p, k, S);
+#pragma unroll
+            for (int v = 0; v < V; ++v) A[v] = 0.f;
+          }
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            float ga, keep;
+            gate_of(g[k][v], ga, keep);
+            S[v] = ga * (S[v] + d[k][v]);
+            A[v] *= ga;
+          }
+        }
+      }
+      // the product over the block's groups
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float all = A[v];
+        for (int dd = p.lc; dd < 64; dd <<= 1) all *= __shfl_xor(all, dd, 64);
+        prod[v] *= all;
+      }
+      join_groups<FORWARD>(p, A, S, state, enter);
+    }
+  }
+  if (p.mine == 0) {
+    put_channels(a.map_a + unit * a.dim, p, prod);
+    put_channels(a.map_s + unit * a.dim, p, state);
+  }
+}
+
+// Cut: the ranges' maps to the states that enter them, in place of map_s.  A workgroup takes 4 channels, so that its 256
+// groups of threads walk few ranges each (3,400 ranges of 64 channels: 16 channels and 64 groups took 23 us, most of
+// it waiting for one load after the other); they compose them, join by shuffles and LDS, and walk them again.
+constexpr int kScanThreadsGlr = 1024, kScanChannels = 4, kScanGroups = kScanThreadsGlr / kScanChannels;
+
+template <bool FORWARD>
+__global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs a) {
+  constexpr int kScanWaves = kScanThreadsGlr / 64;
+  __shared__ float la[kScanWaves][kScanChannels], ls[kScanWaves][kScanChannels];
+  const int c = threadIdx.x % kScanChannels, g = threadIdx.x / kScanChannels;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ch = (int)blockIdx.x * kScanChannels + c;
+  const int64_t per = (a.units + kScanGroups - 1) / kScanGroups, begin = min(g * per, a.units), end = min(begin + per, a.units);
+  const auto at = [&](int64_t i) { return (FORWARD ? i : a.units - 1 - i) * a.dim + ch; };
+  // eight ranges' maps in flight
+  const auto walk = [&](auto use) {
+    for (int64_t i0 = begin; i0 < end; i0 += 8) {
+      float ma[8], ms[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t i = min(i0 + u, end - 1);
+        ma[u] = a.map_a[at(i)];
+        ms[u] = a.map_s[at(i)];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u < end) use(i0 + u, ma[u], ms[u]);
+    }
+  };
+  float A = 1.f, S = 0.f, h = 0.f;
+  if (ch < a.dim)
+    walk([&](int64_t, float ma, float ms) {
+      S = mul0(ma, S) + ms;
+      A *= ma;
+    });
+  // the groups of a wave, then the waves
+#pragma unroll
+  for (int d = kScanChannels; d < 64; d <<= 1) {
+    const float s0 = __shfl_up(S, d, 64), a0 = __shfl_up(A, d, 64);
+    if (lane >= d) {
+      S = mul0(A, s0) + S;
+      A *= a0;
+    }
+  }
+  if (lane >= 64 - kScanChannels) {
+    la[wave][c] = A;
+    ls[wave][c] = S;
+  }
+  __syncthreads();
+  for (int i = 0; i < wave; ++i) h = mul0(la[i][c], h) + ls[i][c];
+  const float s0 = __shfl_up(S, kScanChannels, 64), a0 = __shfl_up(A, kScanChannels, 64);
+  if (lane >= kScanChannels) h = mul0(a0, h) + s0;
+  if (ch < a.dim)
+    walk([&](int64_t i, float ma, float ms) {
+      a.map_s[at(i)] = h;
+      h = mul0(ma, h) + ms;
+    });
+}
+
+template <bool WIDE, typename T>
+__global__ __launch_bounds__(kThreads) void glr_step_kernel(const GlrStepArgs a) {
+  const int pieces = (a.dim + V - 1) / V;
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= a.batch * pieces) return;
+  const int64_t b = i / pieces;
+  const int ch = (int)(i % pieces) * V, have = min(V, a.dim - ch);
+  const int64_t slot = a.slots ? a.slots[b] : b;
+  const bool inside = slot >= 0 && slot < a.num_slots;
+  float h[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) h[v] = 0.f;
+  if (inside) {
+    const Elems<T, V> x = load_elems<WIDE, T, V>(static_cast<const T*>(a.x) + b * a.x_stride + ch, have);
+    const Elems<T, V> g = load_elems<WIDE, T, V>(static_cast<const T*>(a.gate) + b * a.gate_stride + ch, have);
+    float* state = a.state + slot * a.dim + ch;
+    const Elems<float, V> s = load_elems<WIDE, float, V>(state, have);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float ga, keep;
+      gate_of(g[v], ga, keep);
+      h[v] = fmaf(ga, s[v], mul0(keep, x[v]));
+    }
+    store_elems<WIDE, float, V>(state, h, have);
+  } else if (ch == 0 && a.status) {
+    atomicOr(a.status, DPI_DEVSTAT_BAD_ID);
+  }
+  store_elems<WIDE, T, V>(static_cast<T*>(a.h) + b * a.h_stride + ch, h, have);
+}
+
+template <bool WIDE, typename T>
+hipError_t run_pass(const GlrArgs& a, bool backward, hipStream_t s) {
+  const GlrShape sh = glr_shape(a.tokens, a.dim);
+  const dim3 grid((unsigned)std::max<int64_t>(1, (a.units + kWaves - 1) / kWaves), (unsigned)sh.channel_blocks);
+  if (!a.cut) {
+    if (backward)
+      glr_backward_kernel<false, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    else
+      glr_forward_kernel<false, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  const dim3 scan((unsigned)((a.dim + kScanChannels - 1) / kScanChannels));
+  if (backward) {
+    glr_maps_kernel<false, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    glr_scan_kernel<false><<<scan, kScanThreadsGlr, 0, s>>>(a);
+    glr_backward_kernel<true, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+  } else {
+    glr_maps_kernel<true, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+    glr_scan_kernel<true><<<scan, kScanThreadsGlr, 0, s>>>(a);
+    glr_forward_kernel<true, WIDE, T><<<grid, kThreads, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_wide(const GlrArgs& a, bool backward, hipStream_t s) {
+  return a.wide ? run_pass<true, T>(a, backward, s) : run_pass<false, T>(a, backward, s);
+}
+
+hipError_t run_by_dtype(const GlrArgs& a, bool backward, hipStream_t s) {
+  if (a.seqs == 0) return hipSuccess;
+  if (a.dtype == DPI_F32) return run_wide<float>(a, backward, s);
+  if (a.dtype == DPI_F16) return run_wide<f16_t>(a, backward, s);
+  return run_wide<bf16_t>(a, backward, s);
+}
+
+template <typename T>
+hipError_t run_step(const GlrStepArgs& a, hipStream_t s) {
+  const int64_t threads = a.batch * ((a.dim + V - 1) / V);
+  const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
+  if (a.wide)
+    glr_step_kernel<true, T><<<grid, kThreads, 0, s>>>(a);
+  else
+    glr_step_kernel<false, T><<<grid, kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Lanes of a power of two cover up to 64 * V channels; a wave's other lanes take later tokens.
+GlrShape glr_shape(int64_t tokens, int32_t dim) {
+  GlrShape sh{};
+  while (sh.lc_log < 6 && (V << sh.lc_log) < dim) ++sh.lc_log;
+  sh.block_tokens = (int64_t)(64 >> sh.lc_log) * K;
+  sh.blocks = (tokens + sh.block_tokens - 1) / sh.block_tokens;
+  sh.channel_blocks = (dim + (V << sh.lc_log) - 1) / (V << sh.lc_log);
+  return sh;
+}
+
+GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len) {
+  const GlrShape sh = glr_shape(tokens, dim);
+  GlrSplit sp{};
+  const int64_t longest = max_len > 0 ? std::min(max_len, tokens) : tokens;
+  sp.cut = longest > kGlrWholeBlocks * sh.block_tokens;
+  const int64_t waves = kGlrWaves / sh.channel_blocks + 1;
+  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (sh.blocks + waves - 1) / waves), kGlrRangeBlocks);
+  sp.range = blocks * sh.block_tokens;
+  sp.units = (tokens + sp.range - 1) / sp.range;
+  return sp;
+}
+
+hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s) { return run_by_dtype(a, false, s); }
+hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s) { return run_by_dtype(a, true, s); }
+
+hipError_t launch_glr_step(const GlrStepArgs& a, hipStream_t s) {
+  if (a.batch == 0) return hipSuccess;
+  if (a.dtype == DPI_F32) return run_step<float>(a, s);
+  if (a.dtype == DPI_F16) return run_step<f16_t>(a, s);
+  return run_step<bf16_t>(a, s);
+}
+
+}  // namespace dpi
