@@ -512,7 +512,7 @@ size_t dpi_glr_workspace_bytes(const dpi_glr_desc* desc);
  * h must not overlap an input.  Malformed offsets set DPI_DEVSTAT_BAD_OFFSETS
  * and leave the outputs unspecified.
  * Errors: INVALID_ARG, UNSUPPORTED (dim > DPI_MAX_DIM, num_tokens or num_seqs
- * >= 2^31, a row stride >= 2^20), MISALIGNED, WORKSPACE_TOO_SMALL, HIP.
+ * >= 2^31, a row stride >= 2^18), MISALIGNED, WORKSPACE_TOO_SMALL, HIP.
  */
 dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, float* h_last, void* entry,
                            void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream);

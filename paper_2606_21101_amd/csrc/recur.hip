@@ -4,21 +4,24 @@
 //   a_t = sigmoid(gate_t),   h_t = a_t h_{t-1} + (1 - a_t) x_t   per channel.
 //
 // A step is the map h -> A h + S; maps compose: (A2, S2) after (A1, S1) is
-// (A2 A1, A2 S1 + S2).  A wave walks a range of tokens a block at a time: LC
-// lanes cover the channels, V each, and the wave's 64 / LC groups of lanes take
-// K tokens each.  A thread composes its K tokens in registers, groups join
-// their maps by shuffles, and each thread walks its tokens again from the state
-// that enters them.  Waves share nothing, so nothing waits for a barrier.
+// (A2 A1, A2 S1 + S2).  A workgroup walks a range of tokens a block at a time:
+// LC lanes cover the channels, V each, and the 64 / LC groups of lanes of each
+// of its 4 waves take K tokens each.  A thread composes its K tokens in
+// registers, groups join their maps by shuffles, waves by LDS, and each thread
+// walks its tokens again from the state that enters them.
 //
 // A sequence's first token is the map with A = 0.  Products with such an A are
 // legacy ones, where 0 times anything is 0: no infinity and no NaN of one
 // sequence gets into the next.  So is (1 - a) x, where a token of gate +inf
 // keeps the state whatever x it has.
 //
-// Work is split in one of two ways.  Whole: a wave takes the sequences that
-// begin in its range of tokens, to their ends; one launch.  Cut: a wave takes
-// its range's tokens only; a first launch composes each range's map, a second
-// scans the maps, a third walks the ranges from the states that enter them.
+// Work is split in one of two ways.  Whole: a workgroup takes the sequences that
+// begin in its range of tokens, to their ends; one launch.  Cut: a workgroup
+// takes its range's tokens only; a first launch composes each range's map, a
+// second scans the maps, a third walks the ranges from the states that enter
+// them.  (Ranges of single waves left the longest sequences to be waited for:
+// 16,384 histories of 27 tokens on average and 256 at most, 128 channels bf16,
+// took 127 us forward where ranges of equal length take 74.)
 //
 // The backward pass runs c_t = a_t (dh_t + c_{t+1}) the same way from the end,
 // c_t being the gradient of h_{t-1}, and computes the states again in fp32 from
@@ -35,16 +38,18 @@ namespace {
 
 constexpr int V = kGlrV, K = kGlrK, kThreads = kGlrThreads, kWaves = kThreads / 64;
 
-// A wave's part of the workgroup's LDS: the sequences that begin and end at a block's tokens, where marked, and K slots of
-// V channels for each lane.
+// LDS of a workgroup.  A wave's own: the sequences that begin and end at its tokens of a block, where marked, and K slots
+// of V channels for each lane.  Shared: two buffers of the waves' maps.
 struct Place;
 struct Scratch {
   int32_t *starts_at, *ends_at;
-  float* slots;
+  float *slots, *maps;
   __device__ __forceinline__ explicit Scratch(const Place& p);
 };
 constexpr int kSlotBytes = K * 64 * V * 4;
-inline size_t scratch_bytes(int64_t block_tokens) { return kWaves * (kSlotBytes + 2 * (size_t)block_tokens * 4); }
+inline size_t scratch_bytes(int lc_log) {
+  return kWaves * (kSlotBytes + 2 * (size_t)(64 >> lc_log) * K * 4) + 2 * 2 * kWaves * ((size_t)V << lc_log) * 4;
+}
 
 // Product in which 0 times anything is 0.
 __device__ __forceinline__ float mul0(float a, float b) {
@@ -61,31 +66,64 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& keep) {
   keep = e * a;
 }
 
-// First s in [0, seqs] with offsets[s + 1] > t, by the whole wave: the sequence that holds token t when the offsets are
-// sound.
-__device__ __forceinline__ int64_t sequence_of(const GlrArgs& a, int64_t t, int lane) {
-  int64_t lo = 0, count = a.seqs;   // the answer lies in [lo, lo + count]
-  while (count > 0) {
-    const int64_t step = (count + 63) >> 6, at = lo + (lane + 1) * step - 1;   // 64 candidates, the last of each part
-    const bool before = at < lo + count && (int64_t)a.offsets[at + 1] <= t;
-    const int parts = __popcll(__ballot(before));
-    lo += parts * step;
-    count = min(step - 1, max(count - parts * step, (int64_t)0));
+__device__ __forceinline__ int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return min(max(x, lo), hi); }
+
+// The first sequence s that ends after token t (offsets[s + 1] > t: the one that holds t when the offsets are sound) and
+// its end; s = seqs without one.
+struct Found {
+  int64_t seq, end;
+};
+
+// N such searches at once, by the whole wave: 256 candidates of each a round, so 65,536 sequences take two trips to memory.
+template <int N>
+__device__ __forceinline__ void find_sequences(const GlrArgs& a, const int64_t* t, int lane, Found* f) {
+  int32_t lo[N], count[N];   // the answer lies in [lo, lo + count), or is seqs
+#pragma unroll
+  for (int n = 0; n < N; ++n) lo[n] = 0, count[n] = (int32_t)a.seqs, f[n].seq = a.seqs, f[n].end = 0;
+  for (bool more = true; more;) {
+    more = false;
+    int32_t got[N][4];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const uint32_t step = ((uint32_t)count[n] + 255) >> 8;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t past = min((uint32_t)(u * 64 + lane + 1) * step, (uint32_t)count[n]);   // past the last of each part
+        got[n][u] = count[n] > 0 ? a.offsets[(int64_t)lo[n] + past] : 0;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (count[n] == 0) continue;
+      const int32_t step = (int32_t)(((uint32_t)count[n] + 255) >> 8);
+      int32_t parts = 0;   // parts that lie before the answer
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        parts += __popcll(__ballot((u * 64 + lane) * step < count[n] && (int64_t)got[n][u] <= t[n]));
+      const int64_t left = count[n] - (int64_t)parts * step;
+      if (left <= 0) {   // none
+        count[n] = 0;
+      } else if (step == 1) {
+        int32_t end = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (parts >> 6 == u) end = __builtin_amdgcn_readlane(got[n][u], parts & 63);
+        f[n].seq = lo[n] + parts;
+        f[n].end = end;
+        count[n] = 0;
+      } else {
+        lo[n] += parts * step;
+        count[n] = (int32_t)min((int64_t)step, left);
+        more = true;
+      }
+    }
   }
-  return __builtin_amdgcn_readfirstlane((int32_t)lo);
 }
 
-// A wave's tokens [lo, hi), and the sequence that holds the first (forwards) or the last of them (backwards).
+// A workgroup's tokens [lo, hi), and the sequence that holds the first (forwards) or the last of them (backwards).
 struct Span {
   int64_t lo, hi, seq;
 };
-
-__device__ __forceinline__ int64_t clamped(int64_t x, int64_t lo, int64_t hi) { return min(max(x, lo), hi); }
-
-// The same for the whole wave.
-__device__ __forceinline__ int64_t offset_at(const GlrArgs& a, int64_t s) {
-  return __builtin_amdgcn_readfirstlane(a.offsets[s]);
-}
 
 // Whole: from the first sequence start at or after the range's begin to the end of the last sequence begun before its
 // end.
@@ -98,15 +136,19 @@ __device__ __forceinline__ Span span_of(const GlrArgs& a, int64_t unit, int lane
   s.seq = 0;
   if (t0 >= t1) return s;
   if (CUT) {
-    s.seq = sequence_of(a, FORWARD ? t0 : t1 - 1, lane);
+    Found f;
+    const int64_t t = FORWARD ? t0 : t1 - 1;
+    find_sequences<1>(a, &t, lane, &f);
+    s.seq = f.seq;
     return s;
   }
-  const int64_t first = t0 > 0 ? sequence_of(a, t0 - 1, lane) : -1;
-  const int64_t last = sequence_of(a, t1 - 1, lane);
-  if (t0 > 0) s.lo = first < a.seqs ? clamped(offset_at(a, first + 1), t0, a.tokens) : a.tokens;
-  s.hi = last < a.seqs ? clamped(offset_at(a, last + 1), t1, a.tokens) : a.tokens;
+  Found f[2];
+  const int64_t t[2] = {t0 - 1, t1 - 1};
+  find_sequences<2>(a, t, lane, f);
+  if (t0 > 0) s.lo = f[0].seq < a.seqs ? clamped(f[0].end, t0, a.tokens) : a.tokens;
+  s.hi = f[1].seq < a.seqs ? clamped(f[1].end, t1, a.tokens) : a.tokens;
   if (s.lo >= t1) s.hi = s.lo;   // no sequence begins in the range
-  s.seq = FORWARD ? max(first, (int64_t)0) : last;
+  s.seq = FORWARD ? f[0].seq : f[1].seq;
   return s;
 }
 
@@ -188,10 +230,10 @@ __device__ __forceinline__ void share_of_sequences(const GlrArgs& a, const float
   if (bad && a.status) atomicOr(a.status, DPI_DEVSTAT_BAD_OFFSETS);
 }
 
-// What a thread knows of its place: lane c of LC covers channels [ch, ch + V), its group tokens [mine, mine + K) of a
-// block.
+// What a thread knows of its place: lane c of LC covers channels [ch, ch + V), its group the tokens [mine, mine + K) of its
+// wave's `tokens`, which are rows [row, row + K) of the workgroup's block of `rows`.
 struct Place {
-  int lane, wave, lc, c, mine, tokens, ch, have;   // have: channels that exist, 0 for none
+  int lane, wave, lc, c, mine, row, tokens, rows, ch, have;   // have: channels that exist, 0 for none
 };
 
 __device__ __forceinline__ Place place_of(const GlrArgs& a) {
@@ -202,6 +244,8 @@ __device__ __forceinline__ Place place_of(const GlrArgs& a) {
   p.c = p.lane & (p.lc - 1);
   p.mine = (p.lane >> a.lc_log) * K;
   p.tokens = (64 >> a.lc_log) * K;
+  p.rows = kWaves * p.tokens;
+  p.row = p.wave * p.tokens + p.mine;
   p.ch = ((int)blockIdx.y * p.lc + p.c) * V;
   p.have = max(0, min(V, a.dim - p.ch));
   return p;
@@ -210,25 +254,36 @@ __device__ __forceinline__ Place place_of(const GlrArgs& a) {
 __device__ __forceinline__ Scratch::Scratch(const Place& p) {
   extern __shared__ __align__(16) char lds[];
   slots = reinterpret_cast<float*>(lds) + p.wave * (kSlotBytes / 4);
-  starts_at = reinterpret_cast<int32_t*>(lds + kWaves * kSlotBytes) + p.wave * 2 * p.tokens;
+  maps = reinterpret_cast<float*>(lds + kWaves * kSlotBytes);
+  starts_at = reinterpret_cast<int32_t*>(maps + 4 * kWaves * V * p.lc) + p.wave * 2 * p.tokens;
   ends_at = starts_at + p.tokens;
 }
 
-__device__ __forceinline__ void put_channels(float* row, const Place& p, const float* v) {
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i < p.have) row[p.ch + i] = v[i];
+// A thread's channels of a row of fp32 states.  WIDE: rows are 16-byte aligned, of whole pieces.
+template <bool WIDE>
+__device__ __forceinline__ void put_channels(float* states, int64_t row, const GlrArgs& a, const Place& p, const float* v) {
+  float* at = states + row * a.dim + p.ch;
+  if (p.have > 0) store_elems<WIDE, float, V>(at, v, p.have);
 }
 
-// A wave's place in its span: the block at token t0, whose rows [first, past) belong to the span.
+template <bool WIDE>
+__device__ __forceinline__ void get_channels(const float* states, int64_t row, const GlrArgs& a, const Place& p, float* v) {
+  if (p.have > 0) {
+    const Elems<float, V> e = load_elems<WIDE, float, V>(states + row * a.dim + p.ch, p.have);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = e[i];
+  }
+}
+
+// A workgroup's place in its span: the block at token t0, whose rows [first, past) belong to the span.
 struct Block {
   int64_t t0;
   int32_t first, past;
   bool whole;
 
   __device__ __forceinline__ Block(const Place& p, int64_t t, int64_t lo, int64_t hi)
-      : t0(t), first((int32_t)max(lo - t, (int64_t)0)), past((int32_t)min(hi - t, (int64_t)p.tokens)) {
-    whole = first == 0 && past == p.tokens;
+      : t0(t), first((int32_t)max(lo - t, (int64_t)0)), past((int32_t)min(hi - t, (int64_t)p.rows)) {
+    whole = first == 0 && past == p.rows;
   }
   __device__ __forceinline__ bool has(int32_t row) const { return whole || (row >= first && row < past); }
 };
@@ -247,7 +302,7 @@ struct Rows {
     rsrc = __builtin_amdgcn_make_buffer_rsrc(
         static_cast<char*>(const_cast<void*>(p)) + b.t0 * row_stride * (int64_t)sizeof(T), (short)0, b.past * stride, 0x00020000);
     // a thread without channels reads the row's first ones
-    lane = at.mine * stride + (at.have > 0 ? at.ch * (int32_t)sizeof(T) : 0);
+    lane = at.row * stride + (at.have > 0 ? at.ch * (int32_t)sizeof(T) : 0);
   }
   __device__ __forceinline__ Elems<T, V> get(int k) const {
     Elems<T, V> e;
@@ -307,7 +362,7 @@ __device__ __forceinline__ void load_block(const void* from, int64_t stride, con
   if (b.whole) return;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    if (b.has(p.mine + k)) continue;
+    if (b.has(p.row + k)) continue;
 #pragma unroll
     for (int v = 0; v < V; ++v) e[k].raw[v] = (T)other;
   }
@@ -326,18 +381,11 @@ __device__ __forceinline__ void load_dh(const GlrArgs& a, const Place& p, const 
   }
 }
 
-// Groups' maps (A, S) to the state that enters the thread's tokens, `enter`; `state`, the one that enters the block,
-// becomes the one that leaves it.  UP: groups in order of time, else against it.
+// Threads' maps (A, S) to the state that enters each one's tokens, `enter`; `state`, the one that enters the block, becomes
+// the one that leaves it.  UP: groups and waves in order of time, else against it.  maps: a buffer that no thread has to
+// read any more when another comes here.
 template <bool UP>
-__device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, float* state, float* enter) {
-  const bool first = UP ? p.lane < p.lc : p.lane >= 64 - p.lc;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    if (first) {   // from here on its map forgets what came before it
-      S[v] = mul0(A[v], state[v]) + S[v];
-      A[v] = 0.f;
-    }
-  }
+__device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, float* maps, float* state, float* enter) {
   for (int d = p.lc; d < 64; d <<= 1) {
     const bool has = UP ? p.lane >= d : p.lane + d < 64;
 #pragma unroll
@@ -350,18 +398,34 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
       }
     }
   }
+  const bool last = UP ? p.lane >= 64 - p.lc : p.lane < p.lc;
+  float* const all_a = maps + p.c * V;
+  float* const all_s = all_a + kWaves * V * p.lc;
+  if (last) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      all_a[p.wave * V * p.lc + v] = A[v];
+      all_s[p.wave * V * p.lc + v] = S[v];
+    }
+  }
+  __syncthreads();
+  float mine[V];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    const int w = UP ? i : kWaves - 1 - i;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (w == p.wave) mine[v] = state[v];
+      state[v] = mul0(all_a[w * V * p.lc + v], state[v]) + all_s[w * V * p.lc + v];
+    }
+  }
+  const bool first = UP ? p.lane < p.lc : p.lane >= 64 - p.lc;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const float s0 = UP ? __shfl_up(S[v], p.lc & 63, 64) : __shfl_down(S[v], p.lc & 63, 64);
-    enter[v] = first ? state[v] : s0;
-    state[v] = __shfl(S[v], UP ? 64 - p.lc + p.c : p.c, 64);
+    const float a0 = UP ? __shfl_up(A[v], p.lc & 63, 64) : __shfl_down(A[v], p.lc & 63, 64);
+    enter[v] = first ? mine[v] : mul0(a0, mine[v]) + s0;
   }
-}
-
-// A thread's part of a row of states (zeros without them): what a sequence begins (ends) with.
-__device__ __forceinline__ void edge_state(const float* states, const GlrArgs& a, const Place& p, int32_t seq, float* out) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) out[v] = states && v < p.have ? states[(int64_t)seq * a.dim + p.ch + v] : 0.f;
 }
 
 // The edges among a thread's tokens.  The first one's state is in registers, read as soon as the marks are known with the
@@ -372,20 +436,24 @@ struct Edges {
   float state[V];
   const float* extra;  // [K][64][V], the thread's column
 
+  template <bool WIDE>
   __device__ __forceinline__ void read(const GlrArgs& a, const Place& p, uint32_t m, const int32_t* seqs, const float* from) {
     mask = m;
     k = m ? __builtin_ctz(m) : 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) state[v] = 0.f;
-    if (m && from) edge_state(from, a, p, seqs[p.mine + k], state);
+    if (m && from) get_channels<WIDE>(from, seqs[p.mine + k], a, p, state);
   }
   // Not before the last use of what the slots held.
+  template <bool WIDE>
   __device__ __forceinline__ void read_more(const GlrArgs& a, const Place& p, const int32_t* seqs, const float* from, float* slots) {
     extra = slots + p.lane * V;
     for (uint32_t m = mask & (mask - 1); m; m &= m - 1) {
       const int i = __builtin_ctz(m);
       float more[V];
-      edge_state(from, a, p, seqs[p.mine + i], more);
+#pragma unroll
+      for (int v = 0; v < V; ++v) more[v] = 0.f;
+      if (from) get_channels<WIDE>(from, seqs[p.mine + i], a, p, more);
 #pragma unroll
       for (int v = 0; v < V; ++v) slots[(i * 64 + p.lane) * V + v] = more[v];
     }
@@ -421,8 +489,8 @@ __device__ __forceinline__ void next_phase(Elems<T, V>* e) {
 // The maps h -> fa h + b of a thread's tokens, b = keep x, and their composition (A, S).  A sequence's first token starts
 // from its h0 and forgets the rest.  KEEP: the keeps instead of the b's.
 template <bool KEEP, typename T>
-__device__ __forceinline__ void compose(const GlrArgs& a, const Place& p, const Elems<T, V>* x, const Elems<T, V>* g,
-                                        const Edges& begin, float (*fa)[V], float (*fb)[V], float* A, float* S) {
+__device__ __forceinline__ void compose(const Elems<T, V>* x, const Elems<T, V>* g, const Edges& begin, float (*fa)[V],
+                                        float (*fb)[V], float* A, float* S) {
 #pragma unroll
   for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
 #pragma unroll
@@ -447,148 +515,133 @@ __device__ __forceinline__ void compose(const GlrArgs& a, const Place& p, const 
 template <bool CUT, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads) void glr_forward_kernel(const GlrArgs a) {
   const Place p = place_of(a);
-  share_of_sequences(a, a.h0, a.h_last);
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
-  const Span s = span_of<CUT, true>(a, unit, p.lane);
-  if (s.lo >= s.hi) return;
-  const Scratch lds(p);
-  int32_t *starts_at = lds.starts_at, *ends_at = lds.ends_at;
-  float* slots = lds.slots;
-  Window w;
-  w.load(a, s.seq, p.lane);
-  float state[V];
+  const Span s = span_of<CUT, true>(a, blockIdx.x, p.lane);   // the same in every wave
+  if (s.lo < s.hi) {
+    const Scratch lds(p);
+    Window w;
+    w.load(a, s.seq, p.lane);
+    float state[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) state[v] = CUT && v < p.have ? a.map_s[unit * a.dim + p.ch + v] : 0.f;
-  for (int64_t block = s.lo / p.tokens; block * p.tokens < s.hi; ++block) {
-    const int64_t t0 = block * p.tokens;
-    const Block bl(p, t0, s.lo, s.hi);
-    Elems<T, V> x[K], g[K];
-    load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
-    load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);   // a token outside keeps the state
-    uint32_t starts, ends;
-    marks_of<true>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, starts_at, ends_at, starts, ends);
-    if (a.entry && t0 >= s.lo && p.mine == 0) put_channels(a.entry + block * a.dim, p, state);
-    Edges begin;
-    begin.read(a, p, starts, starts_at, a.h0);
-    begin.read_more(a, p, starts_at, a.h0, slots);
-    float fa[K][V], fb[K][V], A[V], S[V], h[V];
-    compose<false, T>(a, p, x, g, begin, fa, fb, A, S);
-    join_groups<true>(p, A, S, state, h);
-    if (p.have == 0) continue;
-    const Rows<WIDE, T> out(a.h, a.h_stride, p, bl);
+    for (int v = 0; v < V; ++v) state[v] = 0.f;
+    if (CUT) get_channels<WIDE>(a.map_s, blockIdx.x, a, p, state);
+    int parity = 0;
+    for (int64_t block = s.lo / p.rows; block * p.rows < s.hi; ++block, parity ^= 1) {
+      const int64_t t0 = block * p.rows;
+      const Block bl(p, t0, s.lo, s.hi);
+      Elems<T, V> x[K], g[K];
+      load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+      load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);   // a token outside keeps the state
+      uint32_t starts, ends;
+      marks_of<true>(a, w, t0 + p.wave * p.tokens, p.tokens, s.lo, s.hi, p.lane, p.mine, lds.starts_at, lds.ends_at, starts, ends);
+      Edges begin;
+      begin.read<WIDE>(a, p, starts, lds.starts_at, a.h0);
+      begin.read_more<WIDE>(a, p, lds.starts_at, a.h0, lds.slots);
+      if (a.entry && t0 >= s.lo && p.row == 0) put_channels<WIDE>(a.entry, block, a, p, state);
+      float fa[K][V], fb[K][V], A[V], S[V], h[V];
+      compose<false, T>(x, g, begin, fa, fb, A, S);
+      join_groups<true>(p, A, S, lds.maps + parity * 2 * kWaves * V * p.lc, state, h);
+      if (p.have == 0) continue;
+      const Rows<WIDE, T> out(a.h, a.h_stride, p, bl);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (begin.is(k)) begin.get(k, h);
+      for (int k = 0; k < K; ++k) {
+        if (begin.is(k)) begin.get(k, h);
 #pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = fmaf(fa[k][v], h[v], fb[k][v]);
-      if (bl.has(p.mine + k)) out.put(k, h);
-      if ((ends >> k & 1) && a.h_last) put_channels(a.h_last + (int64_t)ends_at[p.mine + k] * a.dim, p, h);
+        for (int v = 0; v < V; ++v) h[v] = fmaf(fa[k][v], h[v], fb[k][v]);
+        if (bl.has(p.row + k)) out.put(k, h);
+        if ((ends >> k & 1) && a.h_last) put_channels<WIDE>(a.h_last, lds.ends_at[p.mine + k], a, p, h);
+      }
     }
   }
+  share_of_sequences(a, a.h0, a.h_last);
 }
 
 template <bool CUT, bool WIDE, typename T>
-__global__ __launch_bounds__(kThreads, 2) void glr_backward_kernel(const GlrArgs a) {
+__global__ __launch_bounds__(kThreads, 3) void glr_backward_kernel(const GlrArgs a) {
   const Place p = place_of(a);
-  share_of_sequences(a, a.dh_last, a.dh0);
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
-  const Span s = span_of<CUT, false>(a, unit, p.lane);
-  if (s.lo >= s.hi) return;
-  const Scratch lds(p);
-  Window w;
-  w.load(a, s.seq - 62, p.lane);   // the span's last sequence, or one past it, is the window's last
-  float grad[V];
+  const Span s = span_of<CUT, false>(a, blockIdx.x, p.lane);
+  if (s.lo < s.hi) {
+    const Scratch lds(p);
+    float grad[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) grad[v] = CUT && v < p.have ? a.map_s[unit * a.dim + p.ch + v] : 0.f;
-  // the next block's rows travel while this one's are worked on: two waves a SIMD do not hide the latency by themselves
-  // (rows of fp32 would not fit the registers)
-  constexpr bool AHEAD = sizeof(T) == 2;
-  Elems<T, V> nx[K], ng[K], nd[K];
-  float entering[V];
-  const auto fetch = [&](int64_t block) {
-    const int64_t t0 = block * p.tokens;
-    const Block bl(p, t0, s.lo, s.hi);
-    load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, nx);
-    load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, ng);   // a token outside keeps the state, and the gradient
-    load_dh<WIDE, T>(a, p, bl, nd);
+    for (int v = 0; v < V; ++v) grad[v] = 0.f;
+    if (CUT) get_channels<WIDE>(a.map_s, blockIdx.x, a, p, grad);
+    Window w;
+    w.load(a, s.seq - 62, p.lane);   // the span's last sequence, or one past it, is the window's last
+    for (int64_t block = (s.hi - 1) / p.rows; block >= s.lo / p.rows; --block) {
+      const int64_t t0 = block * p.rows;
+      const Block bl(p, t0, s.lo, s.hi);
+      Elems<T, V> x[K], g[K], d[K];
+      load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
+      load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);   // a token outside keeps the state, and the gradient
+      load_dh<WIDE, T>(a, p, bl, d);
+      float state[V];   // enters the block, if its sequence began before it
 #pragma unroll
-    for (int v = 0; v < V; ++v) entering[v] = t0 >= s.lo && v < p.have ? a.entry[block * a.dim + p.ch + v] : 0.f;
-  };
-  const int64_t last = s.lo / p.tokens;
-  if (AHEAD) fetch((s.hi - 1) / p.tokens);
-  for (int64_t block = (s.hi - 1) / p.tokens; block >= last; --block) {
-    if (!AHEAD) fetch(block);
-    const int64_t t0 = block * p.tokens;
-    const Block bl(p, t0, s.lo, s.hi);
-    uint32_t starts, ends;
-    marks_of<false>(a, w, t0, p.tokens, s.lo, s.hi, p.lane, p.mine, lds.starts_at, lds.ends_at, starts, ends);
-    Edges begin, end;
-    begin.read(a, p, starts, lds.starts_at, a.h0);
-    end.read(a, p, ends, lds.ends_at, a.dh_last);
-    Elems<T, V> x[K], g[K], d[K];
-    float state[V];   // enters the block, if its sequence began before it
+      for (int v = 0; v < V; ++v) state[v] = 0.f;
+      if (t0 >= s.lo) get_channels<WIDE>(a.entry, block, a, p, state);
+      uint32_t starts, ends;
+      marks_of<false>(a, w, t0 + p.wave * p.tokens, p.tokens, s.lo, s.hi, p.lane, p.mine, lds.starts_at, lds.ends_at, starts, ends);
+      Edges begin, end;
+      begin.read<WIDE>(a, p, starts, lds.starts_at, a.h0);
+      end.read<WIDE>(a, p, ends, lds.ends_at, a.dh_last);
+      begin.read_more<WIDE>(a, p, lds.starts_at, a.h0, lds.slots);
+      float fa[K][V], kp[K][V], hx[K][V], A[V], S[V], h[V];
+      compose<true, T>(x, g, begin, fa, kp, A, S);
+      join_groups<true>(p, A, S, lds.maps, state, h);
+      next_phase(x);
+      // the state before each token less its x, which dgate needs
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = nx[k], g[k] = ng[k], d[k] = nd[k];
+      for (int k = 0; k < K; ++k) {
+        if (begin.is(k)) begin.get(k, h);
 #pragma unroll
-    for (int v = 0; v < V; ++v) state[v] = entering[v];
-    if (AHEAD && block > last) fetch(block - 1);
-    begin.read_more(a, p, lds.starts_at, a.h0, lds.slots);
-    float fa[K][V], kp[K][V], hx[K][V], A[V], S[V], h[V];
-    compose<true, T>(a, p, x, g, begin, fa, kp, A, S);
-    join_groups<true>(p, A, S, state, h);
-    next_phase(x);
-    // the state before each token less its x, which dgate needs
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (begin.is(k)) begin.get(k, h);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float xv = x[k][v];
-        hx[k][v] = h[v] - xv;
-        h[v] = fmaf(fa[k][v], h[v], mul0(kp[k][v], xv));
+        for (int v = 0; v < V; ++v) {
+          const float xv = x[k][v];
+          hx[k][v] = h[v] - xv;
+          h[v] = fmaf(fa[k][v], h[v], mul0(kp[k][v], xv));
+        }
       }
-    }
-    next_phase(d);
-    end.read_more(a, p, lds.ends_at, a.dh_last, lds.slots);
-    // the gradients' maps, from the last token on: A and S once more
+      next_phase(d);
+      end.read_more<WIDE>(a, p, lds.ends_at, a.dh_last, lds.slots);
+      // the gradients' maps, from the last token on: A and S once more
 #pragma unroll
-    for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
+      for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
 #pragma unroll
-    for (int k = K - 1; k >= 0; --k) {
-      if (end.is(k)) {
-        end.get(k, S);
+      for (int k = K - 1; k >= 0; --k) {
+        if (end.is(k)) {
+          end.get(k, S);
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 0.f;
+          for (int v = 0; v < V; ++v) A[v] = 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          S[v] = fa[k][v] * (S[v] + d[k][v]);
+          A[v] *= fa[k][v];
+        }
       }
+      float c[V];
+      join_groups<false>(p, A, S, lds.maps + 2 * kWaves * V * p.lc, grad, c);
+      next_phase(d);
+      if (p.have == 0) continue;
+      const Rows<WIDE, T> dx_rows(a.dx, a.dx_stride, p, bl), dgate_rows(a.dgate, a.dgate_stride, p, bl);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        S[v] = fa[k][v] * (S[v] + d[k][v]);
-        A[v] *= fa[k][v];
-      }
-    }
-    float c[V];
-    join_groups<false>(p, A, S, grad, c);
-    next_phase(d);
-    if (p.have == 0) continue;
-    const Rows<WIDE, T> dx_rows(a.dx, a.dx_stride, p, bl), dgate_rows(a.dgate, a.dgate_stride, p, bl);
+      for (int k = K - 1; k >= 0; --k) {
+        float dx[V], dg[V];
+        if (end.is(k)) end.get(k, c);
 #pragma unroll
-    for (int k = K - 1; k >= 0; --k) {
-      float dx[V], dg[V];
-      if (end.is(k)) end.get(k, c);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float e = c[v] + d[k][v];
-        c[v] = fa[k][v] * e;
-        dx[v] = kp[k][v] * e;
-        dg[v] = mul0(kp[k][v], hx[k][v]) * c[v];
+        for (int v = 0; v < V; ++v) {
+          const float e = c[v] + d[k][v];
+          c[v] = fa[k][v] * e;
+          dx[v] = kp[k][v] * e;
+          dg[v] = mul0(kp[k][v], hx[k][v]) * c[v];
+        }
+        if (bl.has(p.row + k)) {
+          dx_rows.put(k, dx);
+          dgate_rows.put(k, dg);
+        }
+        if ((starts >> k & 1) && a.dh0) put_channels<WIDE>(a.dh0, lds.starts_at[p.mine + k], a, p, c);
       }
-      if (bl.has(p.mine + k)) {
-        dx_rows.put(k, dx);
-        dgate_rows.put(k, dg);
-      }
-      if ((starts >> k & 1) && a.dh0) put_channels(a.dh0 + (int64_t)lds.starts_at[p.mine + k] * a.dim, p, c);
     }
   }
+  share_of_sequences(a, a.dh_last, a.dh0);
 }
 
 // Cut: the map of a range's tokens.  Only those after the last sequence start in it (backwards: before the first end)
@@ -596,37 +649,39 @@ __global__ __launch_bounds__(kThreads, 2) void glr_backward_kernel(const GlrArgs
 template <bool FORWARD, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
   const Place p = place_of(a);
-  const int64_t unit = (int64_t)blockIdx.x * kWaves + p.wave;
-  if (unit >= a.units) return;
-  const int64_t lo = min(unit * a.range, a.tokens), hi = min(lo + a.range, a.tokens);
-  const int64_t seq = sequence_of(a, FORWARD ? hi - 1 : lo, p.lane);
-  const int64_t begin = seq < a.seqs ? offset_at(a, seq) : 0, end = seq < a.seqs ? offset_at(a, seq + 1) : hi;
+  const int64_t lo = min(blockIdx.x * a.range, a.tokens), hi = min(lo + a.range, a.tokens);
+  if (lo >= hi) return;
+  Found f;
+  const int64_t edge_token = FORWARD ? hi - 1 : lo;
+  find_sequences<1>(a, &edge_token, p.lane, &f);
+  const int64_t seq = f.seq, end = seq < a.seqs ? f.end : hi;
+  const int64_t begin = seq < a.seqs ? __builtin_amdgcn_readfirstlane(a.offsets[seq]) : 0;
   const int64_t from = FORWARD ? clamped(begin, lo, hi - 1) : lo, to = FORWARD ? hi : clamped(end, lo + 1, hi);
   float A[V], S[V], prod[V], state[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) prod[v] = 1.f, state[v] = 0.f;
   if (FORWARD ? end > hi : begin < lo) {   // the range's edge lies within the sequence
     const Scratch lds(p);
-    int32_t *starts_at = lds.starts_at, *ends_at = lds.ends_at;
     Window w;
     w.load(a, FORWARD ? seq : seq - 62, p.lane);
-    const int64_t b0 = from / p.tokens, b1 = (to - 1) / p.tokens;
-    for (int64_t i = b0; i <= b1; ++i) {
-      const int64_t t0 = (FORWARD ? i : b0 + b1 - i) * p.tokens;
+    const int64_t b0 = from / p.rows, b1 = (to - 1) / p.rows;
+    int parity = 0;
+    for (int64_t i = b0; i <= b1; ++i, parity ^= 1) {
+      const int64_t t0 = (FORWARD ? i : b0 + b1 - i) * p.rows;
       const Block bl(p, t0, from, to);
       Elems<T, V> x[K], g[K], d[K];
       if (FORWARD) load_block<WIDE, T>(a.x, a.x_stride, p, bl, 0.f, x);
       load_block<WIDE, T>(a.gate, a.gate_stride, p, bl, INFINITY, g);
       if (!FORWARD) load_dh<WIDE, T>(a, p, bl, d);
       uint32_t starts, ends;
-      marks_of<FORWARD>(a, w, t0, p.tokens, from, to, p.lane, p.mine, starts_at, ends_at, starts, ends);
+      marks_of<FORWARD>(a, w, t0 + p.wave * p.tokens, p.tokens, from, to, p.lane, p.mine, lds.starts_at, lds.ends_at, starts, ends);
       Edges edge;
-      edge.read(a, p, FORWARD ? starts : ends, FORWARD ? starts_at : ends_at, FORWARD ? a.h0 : a.dh_last);
-      edge.read_more(a, p, FORWARD ? starts_at : ends_at, FORWARD ? a.h0 : a.dh_last, lds.slots);
+      edge.read<WIDE>(a, p, FORWARD ? starts : ends, FORWARD ? lds.starts_at : lds.ends_at, FORWARD ? a.h0 : a.dh_last);
+      edge.read_more<WIDE>(a, p, FORWARD ? lds.starts_at : lds.ends_at, FORWARD ? a.h0 : a.dh_last, lds.slots);
       float enter[V];
       if (FORWARD) {
         float fa[K][V], fb[K][V];
-        compose<false, T>(a, p, x, g, edge, fa, fb, A, S);
+        compose<false, T>(x, g, edge, fa, fb, A, S);
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) A[v] = 1.f, S[v] = 0.f;
@@ -646,19 +701,18 @@ __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
           }
         }
       }
-      // the product over the block's groups
+      float* const maps = lds.maps + parity * 2 * kWaves * V * p.lc;
+      join_groups<FORWARD>(p, A, S, maps, state, enter);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float all = A[v];
-        for (int dd = p.lc; dd < 64; dd <<= 1) all *= __shfl_xor(all, dd, 64);
-        prod[v] *= all;
+      for (int i = 0; i < kWaves; ++i) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) prod[v] *= maps[(i * p.lc + p.c) * V + v];
       }
-      join_groups<FORWARD>(p, A, S, state, enter);
     }
   }
-  if (p.mine == 0) {
-    put_channels(a.map_a + unit * a.dim, p, prod);
-    put_channels(a.map_s + unit * a.dim, p, state);
+  if (p.row == 0) {
+    put_channels<WIDE>(a.map_a, blockIdx.x, a, p, prod);
+    put_channels<WIDE>(a.map_s, blockIdx.x, a, p, state);
   }
 }
 
@@ -754,8 +808,8 @@ __global__ __launch_bounds__(kThreads) void glr_step_kernel(const GlrStepArgs a)
 template <bool WIDE, typename T>
 hipError_t run_pass(const GlrArgs& a, bool backward, hipStream_t s) {
   const GlrShape sh = glr_shape(a.tokens, a.dim);
-  const dim3 grid((unsigned)std::max<int64_t>(1, (a.units + kWaves - 1) / kWaves), (unsigned)sh.channel_blocks);
-  const size_t lds = scratch_bytes(sh.block_tokens);
+  const dim3 grid((unsigned)std::max<int64_t>(1, a.units), (unsigned)sh.channel_blocks);
+  const size_t lds = scratch_bytes(sh.lc_log);
   if (!a.cut) {
     if (backward)
       glr_backward_kernel<false, WIDE, T><<<grid, kThreads, lds, s>>>(a);
@@ -801,11 +855,11 @@ hipError_t run_step(const GlrStepArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Lanes of a power of two cover up to 64 * V channels; a wave's other lanes take later tokens.
+// Lanes of a power of two cover up to 64 * V channels; a workgroup's other lanes take later tokens.
 GlrShape glr_shape(int64_t tokens, int32_t dim) {
   GlrShape sh{};
   while (sh.lc_log < 6 && (V << sh.lc_log) < dim) ++sh.lc_log;
-  sh.block_tokens = (int64_t)(64 >> sh.lc_log) * K;
+  sh.block_tokens = (int64_t)(kThreads >> sh.lc_log) * K;
   sh.blocks = (tokens + sh.block_tokens - 1) / sh.block_tokens;
   sh.channel_blocks = (dim + (V << sh.lc_log) - 1) / (V << sh.lc_log);
   return sh;
@@ -816,8 +870,8 @@ GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len) {
   GlrSplit sp{};
   const int64_t longest = max_len > 0 ? std::min(max_len, tokens) : tokens;
   sp.cut = longest > kGlrWholeBlocks * sh.block_tokens;
-  const int64_t waves = kGlrWaves / sh.channel_blocks + 1;
-  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (sh.blocks + waves - 1) / waves), kGlrRangeBlocks);
+  const int64_t groups = kGlrGroups / sh.channel_blocks + 1;
+  const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (sh.blocks + groups - 1) / groups), kGlrRangeBlocks);
   sp.range = blocks * sh.block_tokens;
   sp.units = (tokens + sp.range - 1) / sp.range;
   return sp;

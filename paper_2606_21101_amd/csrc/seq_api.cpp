@@ -72,7 +72,7 @@ dpi_status check_glr(const dpi_glr_desc* d) {
 
 // Rows of a recurrence's operand: a block of them is addressed with 32-bit offsets.
 dpi_status check_glr_rows(const void* p, int64_t stride, const dpi_glr_desc* d, const char* what) {
-  if (stride >= kGlrMaxStride) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "%s: row stride 2^20 or more", what);
+  if (stride >= kGlrMaxStride) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "%s: row stride 2^18 or more", what);
   return check_rows(p, d->dtype, stride, d->dim, d->num_tokens, what);
 }
 
@@ -89,6 +89,7 @@ struct Wide {
   int elem;
   bool ok;
   Wide(int32_t dtype, int32_t dim) : access((size_t)kGlrV * elem_size(dtype)), elem(elem_size(dtype)), ok(dim % kGlrV == 0) {}
+  void states(const float* p) { ok = ok && !off_by(p, 16); }
   void add(const void* p, int64_t stride) { ok = ok && !off_by(p, access) && ((size_t)stride * elem) % access == 0; }
 };
 
@@ -258,6 +259,9 @@ dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, 
   w.add(desc->x, desc->x_stride);
   w.add(desc->gate, desc->gate_stride);
   w.add(h, h_stride);
+  w.states(desc->h0);
+  w.states(h_last);
+  w.states(a.entry);
   a.wide = w.ok;
   const hipError_t e = launch_glr_forward(a, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "recurrence launch");
@@ -293,6 +297,10 @@ dpi_status dpi_glr_backward(const dpi_glr_desc* desc, const void* entry, const v
   if (dh) w.add(dh, dh_stride);
   w.add(dx, dx_stride);
   w.add(dgate, dgate_stride);
+  w.states(desc->h0);
+  w.states(a.entry);
+  w.states(dh_last);
+  w.states(dh0);
   a.wide = w.ok;
   const hipError_t e = launch_glr_backward(a, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "recurrence gradient launch");
@@ -328,7 +336,8 @@ dpi_status dpi_glr_step(const void* x, int64_t x_stride, const void* gate, int64
   w.add(x, x_stride);
   w.add(gate, gate_stride);
   w.add(h, h_stride);
-  a.wide = w.ok && !off_by(state, 16);
+  w.states(state);
+  a.wide = w.ok;
   const hipError_t e = launch_glr_step(a, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? DPI_OK : dpi_hip_status(e, "recurrence step launch");
 }

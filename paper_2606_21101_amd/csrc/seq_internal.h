@@ -75,19 +75,19 @@ struct GlrArgs {
   int32_t dim, dtype;
   int32_t wide;           // every row is aligned to a thread's whole access
   int32_t lc_log;         // log2 of the lanes that cover a block of channels
-  int32_t cut;            // ranges cut sequences (else a wave takes whole ones)
-  int64_t range, units;   // tokens of a wave's range, and ranges
+  int32_t cut;            // ranges cut sequences (else a workgroup takes whole ones)
+  int64_t range, units;   // tokens of a workgroup's range, and ranges
   float* map_a;           // cut: [units][dim], a range's map, then
   float* map_s;           //      ... the state that enters it
 };
 
 constexpr int kGlrThreads = 256;
 constexpr int kGlrV = 4;              // channels per thread
-constexpr int kGlrK = 8;              // tokens per thread
-constexpr int64_t kGlrMaxStride = 1 << 20;   // row strides are smaller: 64 * kGlrK rows span less than 2^31 bytes
-constexpr int kGlrWaves = 4096;       // waves a pass is split into, while ...
+constexpr int kGlrK = 4;              // tokens per thread
+constexpr int64_t kGlrMaxStride = 1 << 18;   // row strides are smaller: kGlrThreads * kGlrK rows span less than 2^31 bytes
+constexpr int kGlrGroups = 1024;      // workgroups a pass is split into, while ...
 constexpr int kGlrRangeBlocks = 16;   // ... a range has at most so many blocks
-constexpr int kGlrWholeBlocks = 32;   // the longest sequence that one wave walks, in blocks
+constexpr int kGlrWholeBlocks = 16;   // the longest sequence that one workgroup walks, in blocks
 
 struct GlrShape {
   int32_t lc_log;
