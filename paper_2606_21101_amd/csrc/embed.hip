@@ -5,13 +5,17 @@
 // elements.  The bound is HBM: distinct rows read, token rows written.
 //
 // Backward: dE[v] = scale * sum_{i: ids[i] = v} dout[i].  Tokens are sorted by
-// id (least significant digit first, stable, so equal ids stay in token order);
-// a group of lanes then adds the rows of kSumChunk sorted tokens and writes
-// each row of the gradient that begins and ends among them.  A row cut by
-// chunk borders leaves a part per chunk, and a second kernel adds those in
-// order: no float atomics, so the sums do not depend on timing.
+// id (least significant digit first, stable, so equal ids stay in token order).
+// A workgroup then sums a span of sorted tokens: a group of LPR lanes adds the
+// rows of a chunk, eight in flight, and writes each row of the gradient that
+// begins and ends in it; rows cut by chunk borders are joined in LDS, those cut
+// by span borders by a second kernel.  Every sum has a fixed order and there
+// are no float atomics, so the result does not depend on timing.  The rows
+// without tokens are zeroed by workgroups of the sort's launches, which leave
+// the memory idle otherwise.  The bound is HBM: dout read, the gradient written.
 #include "elem.h"
 #include "seq_internal.h"
+#include "wave_scan.h"
 
 #include <algorithm>
 
@@ -63,72 +67,136 @@ __device__ __forceinline__ uint32_t key_of(const EmbedGradArgs& a, int64_t i, bo
   return pad || !inside ? (uint32_t)a.num_rows : (uint32_t)id;   // num_rows: after every row, in no row's sum
 }
 
+// Share `share` of a.launches of the gradient set to zero by `blocks` workgroups, of which this is `block`.
+__device__ __forceinline__ void zero_share(const EmbedGradArgs& a, int share, int64_t block, int64_t blocks) {
+  typedef int quad __attribute__((ext_vector_type(4)));
+  const int64_t bytes = a.num_rows * a.dim * (a.grad_dtype == DPI_F32 ? 4 : 2);
+  const int64_t step = blocks * blockDim.x, me = block * blockDim.x + threadIdx.x;
+  const int64_t quads = (reinterpret_cast<uintptr_t>(a.grad) & 15) == 0 ? bytes / 16 : 0;
+  const int64_t end = quads * (share + 1) / a.launches;
+  for (int64_t i = quads * share / a.launches + me; i < end; i += step) static_cast<quad*>(a.grad)[i] = quad{0, 0, 0, 0};
+  if (share == 0)   // what 16-byte stores cannot reach
+    for (int64_t i = quads * 8 + me; i < bytes / 2; i += step) static_cast<uint16_t*>(a.grad)[i] = 0;
+}
+
+// Exclusive prefix over the workgroup of one value a thread; *total: their sum.  sums: a word a wave, free to use.
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t* sums, uint32_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t incl = wave_incl_scan32(x, lane);
+  if (lane == 63) sums[wave] = incl;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    if (w < wave) before += sums[w];
+    all += sums[w];
+  }
+  *total = all;
+  return before + incl - x;
+}
+
+// A wave's item of each lane to its place among the wave's items of the same digit: where the digit's next one goes,
+// counted on.  Lanes that are not live have no place.
+__device__ __forceinline__ uint32_t place_of_digit(uint32_t digit, bool live, int bits, int lane, uint32_t* next) {
+  uint64_t same = __ballot(live);   // lanes with this lane's digit
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot((digit >> b) & 1);
+    same &= (digit >> b) & 1 ? set : ~set;
+  }
+  const int rank = __popcll(same & ((1ull << lane) - 1));
+  const uint32_t at = live ? next[digit] + rank : 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // every lane has read before one counts on
+  if (live && rank == 0) next[digit] += (uint32_t)__popcll(same);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return at;
+}
+
+template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const EmbedGradArgs a, int pass) {
   __shared__ uint32_t count[1 << kSortMaxBits];
+  if (blockIdx.x >= a.tiles) {
+    zero_share(a, 3 * pass, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    return;
+  }
   const int bins = 1 << a.bits, shift = pass * a.bits;
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
+  const int64_t base = (int64_t)blockIdx.x * kSortThreads * ITEMS;
   for (int b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
-  __syncthreads();
   const uint32_t* __restrict__ keys = a.keys[(pass + 1) & 1];
+  uint32_t key[ITEMS];
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u) {
+  for (int u = 0; u < ITEMS; ++u) {
     const int64_t i = base + u * kSortThreads + threadIdx.x;
-    if (i < a.tokens) {
-      const uint32_t key = pass == 0 ? key_of(a, i, true) : keys[i];
-      atomicAdd(&count[(key >> shift) & (bins - 1)], 1u);
-    }
+    key[u] = i < a.tokens ? (pass == 0 ? key_of(a, i, true) : keys[i]) : 0;
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += kSortThreads) a.hist[(int64_t)b * gridDim.x + blockIdx.x] = count[b];
-}
-
-// A wave per digit: its counts over the tiles to their exclusive prefixes, and the digit's total.
-__global__ __launch_bounds__(64) void sort_scan_kernel(const EmbedGradArgs a, int64_t tiles) {
-  uint32_t* h = a.hist + (int64_t)blockIdx.x * tiles;
-  uint32_t sum = 0;
-  for (int64_t i0 = 0; i0 < tiles; i0 += 64) {
-    const int64_t i = i0 + threadIdx.x;
-    const uint32_t c = i < tiles ? h[i] : 0;
-    uint32_t x = c;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t y = (uint32_t)__shfl_up((int)x, d, 64);
-      if ((int)threadIdx.x >= d) x += y;
-    }
-    if (i < tiles) h[i] = sum + x - c;
-    sum += (uint32_t)__shfl((int)x, 63, 64);
-  }
-  if (threadIdx.x == 0) a.total[blockIdx.x] = sum;
+  for (int u = 0; u < ITEMS; ++u)
+    if (base + u * kSortThreads + threadIdx.x < a.tokens) atomicAdd(&count[(key[u] >> shift) & (bins - 1)], 1u);
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += kSortThreads) a.hist[((int64_t)blockIdx.x << a.bits) + b] = count[b];
 }
 
+// The tiles' counts of 64 digits to their exclusive prefixes over the tiles, and the digits' totals: a lane a digit, the
+// 16 waves a range of tiles each.
+constexpr int kSortScanWaves = 16;
+
+__global__ __launch_bounds__(64 * kSortScanWaves) void sort_scan_kernel(const EmbedGradArgs a, int pass) {
+  __shared__ uint32_t sums[kSortScanWaves][64];
+  const int bins = 1 << a.bits, groups = (bins + 63) / 64;
+  if ((int)blockIdx.x >= groups) {
+    zero_share(a, 3 * pass + 1, blockIdx.x - groups, gridDim.x - groups);
+    return;
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int b = blockIdx.x * 64 + lane;
+  const int64_t per = (a.tiles + kSortScanWaves - 1) / kSortScanWaves;
+  const int64_t begin = min(wave * per, a.tiles), end = min(begin + per, a.tiles);
+  const auto walk = [&](auto use) {   // eight tiles' counts in flight
+    for (int64_t t0 = begin; t0 < end; t0 += 8) {
+      uint32_t c[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) c[u] = b < bins ? a.hist[(min(t0 + u, end - 1) << a.bits) + b] : 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (t0 + u < end) use(t0 + u, c[u]);
+    }
+  };
+  uint32_t sum = 0;
+  walk([&](int64_t, uint32_t c) { sum += c; });
+  sums[wave][lane] = sum;
+  __syncthreads();
+  uint32_t at = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kSortScanWaves; ++w) {
+    if (w < wave) at += sums[w][lane];
+    all += sums[w][lane];
+  }
+  if (b >= bins) return;
+  walk([&](int64_t t, uint32_t c) {
+    a.hist[(t << a.bits) + b] = at;
+    at += c;
+  });
+  if (wave == 0) a.total[b] = all;
+}
+
+template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedGradArgs a, int pass) {
-  constexpr int kWaves = kSortThreads / 64;
+  constexpr int kWaves = kSortThreads / 64, kEach = (1 << kSortMaxBits) / kSortThreads;
   __shared__ uint32_t next[kWaves][1 << kSortMaxBits];
-  __shared__ uint32_t start[1 << kSortMaxBits];
+  __shared__ uint32_t sums[kWaves];
+  if (blockIdx.x >= a.tiles) {
+    zero_share(a, 3 * pass + 2, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    return;
+  }
   const int bins = 1 << a.bits, shift = pass * a.bits;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t base = (int64_t)blockIdx.x * kSortTile + wave * 64 * kSortItems;   // a wave's items are consecutive
-  for (int b = threadIdx.x; b < kWaves * bins; b += kSortThreads) next[b / bins][b % bins] = 0;
-  // the digits' starts: an exclusive scan of their totals by the first wave
-  if (wave == 0) {
-    uint32_t sum = 0;
-    for (int b0 = 0; b0 < bins; b0 += 64) {
-      const uint32_t c = b0 + lane < bins ? a.total[b0 + lane] : 0;
-      uint32_t x = c;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = (uint32_t)__shfl_up((int)x, d, 64);
-        if (lane >= d) x += y;
-      }
-      if (b0 + lane < bins) start[b0 + lane] = sum + x - c;
-      sum += (uint32_t)__shfl((int)x, 63, 64);
-    }
-  }
-  uint32_t key[kSortItems], tok[kSortItems];
+  const int64_t base = ((int64_t)blockIdx.x * kWaves + wave) * 64 * ITEMS;   // a wave's items are consecutive
+  uint32_t key[ITEMS], tok[ITEMS];
   const uint32_t* __restrict__ keys = a.keys[(pass + 1) & 1];
   const uint32_t* __restrict__ toks = a.toks[(pass + 1) & 1];
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u) {
+  for (int u = 0; u < ITEMS; ++u) {
     const int64_t i = base + u * 64 + lane;
     key[u] = tok[u] = 0;
     if (i < a.tokens) {
@@ -136,42 +204,129 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedG
       tok[u] = pass == 0 ? (uint32_t)i : toks[i];
     }
   }
-  __syncthreads();
+  // kEach neighbouring digits a thread: where they start, and this tile's part of them
+  uint32_t total[kEach], mine[kEach], sum = 0;
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u)
+  for (int j = 0; j < kEach; ++j) {
+    const int b = threadIdx.x * kEach + j;
+    total[j] = b < bins ? a.total[b] : 0;
+    mine[j] = b < bins ? a.hist[((int64_t)blockIdx.x << a.bits) + b] : 0;
+    sum += total[j];
+  }
+  for (int b = threadIdx.x; b < bins; b += kSortThreads) {
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) next[w][b] = 0;
+  }
+  uint32_t all;
+  uint32_t start = block_prefix<kSortThreads>(sum, sums, &all);   // its barrier also ends the clearing
+#pragma unroll
+  for (int u = 0; u < ITEMS; ++u)
     if (base + u * 64 + lane < a.tokens) atomicAdd(&next[wave][(key[u] >> shift) & (bins - 1)], 1u);
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += kSortThreads) {
-    uint32_t at = start[b] + a.hist[(int64_t)b * gridDim.x + blockIdx.x];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const uint32_t c = next[w][b];
-      next[w][b] = at;
-      at += c;
+  for (int j = 0; j < kEach; ++j) {
+    const int b = threadIdx.x * kEach + j;
+    if (b < bins) {
+      uint32_t at = start + mine[j];
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = next[w][b];
+        next[w][b] = at;
+        at += c;
+      }
     }
+    start += total[j];
   }
   __syncthreads();
   uint32_t* __restrict__ keys_out = a.keys[pass & 1];
   uint32_t* __restrict__ toks_out = a.toks[pass & 1];
 #pragma unroll
-  for (int u = 0; u < kSortItems; ++u) {
+  for (int u = 0; u < ITEMS; ++u) {
     const bool live = base + u * 64 + lane < a.tokens;
-    const uint32_t digit = (key[u] >> shift) & (bins - 1);
-    // lanes with this lane's digit
-    uint64_t same = __ballot(live);
-    for (int b = 0; b < a.bits; ++b) {
-      const uint64_t set = __ballot((digit >> b) & 1);
-      same &= (digit >> b) & 1 ? set : ~set;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
+    const uint32_t at = place_of_digit((key[u] >> shift) & (bins - 1), live, a.bits, lane, next[wave]);
     if (live) {
-      const uint32_t at = next[wave][digit] + rank;
       keys_out[at] = key[u];
       toks_out[at] = tok[u];
     }
-    __builtin_amdgcn_wave_barrier();
-    if (live && rank == 0) next[wave][digit] += (uint32_t)__popcll(same);
-    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// A short list, sorted by one workgroup in LDS; the others zero the gradient.
+__global__ __launch_bounds__(kSortOneThreads) void sort_one_kernel(const EmbedGradArgs a) {
+  constexpr int kWaves = kSortOneThreads / 64, kTile = kSortOneThreads * kSortOneItems;
+  constexpr int kEach = (1 << kSortMaxBits) / kSortOneThreads;
+  static_assert(kEach == 1, "a thread a digit");
+  __shared__ uint32_t next[kWaves][1 << kSortMaxBits];
+  __shared__ uint32_t lkey[kTile], ltok[kTile];
+  __shared__ uint32_t sums[kWaves];
+  if (blockIdx.x > 0) {
+    zero_share(a, 0, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  const int bins = 1 << a.bits, n = (int)a.tokens;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, base = wave * 64 * kSortOneItems;
+  uint32_t key[kSortOneItems], tok[kSortOneItems];
+#pragma unroll
+  for (int u = 0; u < kSortOneItems; ++u) {
+    const int i = base + u * 64 + lane;
+    key[u] = i < n ? key_of(a, i, true) : 0;
+    tok[u] = (uint32_t)i;
+  }
+  for (int pass = 0; pass < a.passes; ++pass) {
+    const int shift = pass * a.bits;
+    if ((int)threadIdx.x < bins) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) next[w][threadIdx.x] = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortOneItems; ++u)
+      if (base + u * 64 + lane < n) atomicAdd(&next[wave][(key[u] >> shift) & (bins - 1)], 1u);
+    __syncthreads();
+    uint32_t sum = 0;
+    if ((int)threadIdx.x < bins) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = next[w][threadIdx.x];
+        next[w][threadIdx.x] = sum;
+        sum += c;
+      }
+    }
+    uint32_t all;
+    const uint32_t start = block_prefix<kSortOneThreads>(sum, sums, &all);
+    if ((int)threadIdx.x < bins) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) next[w][threadIdx.x] += start;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortOneItems; ++u) {
+      const bool live = base + u * 64 + lane < n;
+      const uint32_t at = place_of_digit((key[u] >> shift) & (bins - 1), live, a.bits, lane, next[wave]);
+      if (live) {
+        lkey[at] = key[u];
+        ltok[at] = tok[u];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortOneItems; ++u) {
+      const int i = base + u * 64 + lane;
+      if (i < n) {
+        key[u] = lkey[i];
+        tok[u] = ltok[i];
+      }
+    }
+  }
+  uint32_t* __restrict__ keys_out = a.keys[(a.passes + 1) & 1];
+  uint32_t* __restrict__ toks_out = a.toks[(a.passes + 1) & 1];
+#pragma unroll
+  for (int u = 0; u < kSortOneItems; ++u) {
+    const int i = base + u * 64 + lane;
+    if (i < n) {
+      keys_out[i] = key[u];
+      toks_out[i] = tok[u];
+    }
   }
 }
 
@@ -190,79 +345,170 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& a, uint32_t row, 
     store_elems<true, bf16_t, V>(static_cast<bf16_t*>(a.grad) + at, v, V);
 }
 
+// How a launch covers the sorted tokens: groups of 2^lpr_log lanes take `chunk` of them each, a workgroup's a span.
+struct SumShape {
+  int32_t lpr_log, chunk;
+  int64_t span, spans;
+};
+
+// Where a chunk's first row comes from and its last goes to.
+constexpr uint32_t kRowCut = 1;       // the first row began before the chunk: its part is the chunk's `head`
+constexpr uint32_t kRowGoesOn = 2;    // the last row, begun in the chunk, goes on after it: its part is the `tail`
+constexpr uint32_t kRowThrough = 4;   // one row, begun before the chunk, goes on after it: its part is the `head`
+
 template <typename TIN, int V>
-__global__ __launch_bounds__(kThreads) void embed_sum_kernel(const EmbedGradArgs a, int lpr_log, int64_t chunks) {
-  const int lpr = 1 << lpr_log;
-  const int64_t chunk = (int64_t)blockIdx.x * (kThreads >> lpr_log) + (threadIdx.x >> lpr_log);
+__global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradArgs a, const SumShape sh) {
+  __shared__ float head[kSumThreads * V], tail[kSumThreads * V];   // a thread's own V at [V * thread]
+  __shared__ uint32_t state[kSumThreads];                          // of each group
+  const int lpr = 1 << sh.lpr_log, groups = kSumThreads >> sh.lpr_log, g = threadIdx.x >> sh.lpr_log;
   const int col = ((int)blockIdx.y * lpr + ((int)threadIdx.x & (lpr - 1))) * V;
-  if (chunk >= chunks || col >= a.dim) return;
   const uint32_t* __restrict__ keys = a.keys[(a.passes + 1) & 1];
   const uint32_t* __restrict__ toks = a.toks[(a.passes + 1) & 1];
   const TIN* __restrict__ dout = static_cast<const TIN*>(a.dout);
   const uint32_t none = (uint32_t)a.num_rows;
-  const int64_t begin = chunk * kSumChunk, end = min(begin + kSumChunk, a.tokens);
+  const int64_t begin = (int64_t)blockIdx.x * sh.span + g * sh.chunk, end = min(begin + sh.chunk, a.tokens);
+  const bool mine = col < a.dim;
   float acc[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) acc[j] = 0.f;
-  uint32_t row = keys[begin];
-  bool cut = begin > 0 && keys[begin - 1] == row;   // the row began before this chunk
-  for (int64_t i = begin; i < end && row != none; ++i) {
-    const Elems<TIN, V> e = load_elems<true, TIN, V>(dout + (int64_t)toks[i] * a.dout_stride + col, V);
+  uint32_t how = 0, row = none, last_row = none;
+  if (begin < end) {
+    row = keys[begin];
+    bool cut = row != none && begin > 0 && keys[begin - 1] == row;
+    if (cut) how |= kRowCut;
+    for (int64_t i0 = begin; i0 < end && row != none; i0 += 8) {
+      uint32_t key[9], tok[8];
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += e[j];
-    const uint32_t after = i + 1 < a.tokens ? keys[i + 1] : none;
-    if (after == row && i + 1 < end) continue;
-    if (cut || after == row) {   // a part of the row: its first piece is a chunk's second, every other a chunk's first
-      float* part = a.part + (chunk * 2 + (cut ? 0 : 1)) * a.dim + col;
+      for (int u = 0; u < 8; ++u) {
+        tok[u] = toks[min(i0 + u, a.tokens - 1)];
+        key[u] = keys[min(i0 + u, a.tokens - 1)];
+      }
+      key[8] = i0 + 8 < a.tokens ? keys[i0 + 8] : none;
+      Elems<TIN, V> e[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (mine && i0 + u < end && key[u] != none) e[u] = load_elems<true, TIN, V>(dout + (int64_t)tok[u] * a.dout_stride + col, V);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t i = i0 + u;
+        if (i >= end || key[u] == none) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += e[u][j];
+        const bool goes_on = i + 1 < a.tokens && key[u + 1] == key[u];
+        row = key[u];
+        if (goes_on && i + 1 < end) continue;
+        if (cut) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) head[threadIdx.x * V + j] = acc[j];
+          if (goes_on) how |= kRowThrough;
+        } else if (goes_on) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) tail[threadIdx.x * V + j] = acc[j];
+          how |= kRowGoesOn;
+        } else if (mine) {
+          write_row<V>(a, row, col, acc);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] = 0.f;
+        last_row = row;
+        cut = false;
+        row = i + 1 < a.tokens ? key[u + 1] : none;
+      }
+    }
+  }
+  if ((threadIdx.x & (lpr - 1)) == 0) state[g] = how;
+  __syncthreads();
+  if (!mine) return;
+  // a row that begins in this chunk and goes on: the chunks after it, while it goes through them
+  const bool first = g == 0 && (how & kRowCut);   // ... and one that began before the span
+  if (first) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = head[threadIdx.x * V + j];
+    for (int k = 0; k + 1 < groups && (state[k] & kRowThrough); ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) acc[j] += head[(threadIdx.x + ((k + 1) << sh.lpr_log)) * V + j];
+    }
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.dim + col;
+#pragma unroll
+    for (int j = 0; j < V; ++j) part[j] = acc[j];
+  }
+  if (how & kRowGoesOn) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = tail[threadIdx.x * V + j];
+    bool open = true;
+    for (int k = g + 1; k < groups && open; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) acc[j] += head[(threadIdx.x + ((k - g) << sh.lpr_log)) * V + j];
+      open = (state[k] & kRowThrough) != 0;
+    }
+    if (open) {   // on into the next span
+      float* part = a.part + ((int64_t)blockIdx.x * 2 + 1) * a.dim + col;
 #pragma unroll
       for (int j = 0; j < V; ++j) part[j] = acc[j];
     } else {
-      write_row<V>(a, row, col, acc);
+      write_row<V>(a, last_row, col, acc);
     }
-#pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = 0.f;
-    row = after;
-    cut = false;
   }
 }
 
-// The rows cut by chunk borders: a group of lanes for the chunk in which one begins.
+// The rows cut by span borders: a workgroup for the span in which one begins, its groups of lanes taking turns at the
+// spans after it.
 template <int V>
-__global__ __launch_bounds__(kThreads) void embed_join_kernel(const EmbedGradArgs a, int lpr_log, int64_t chunks) {
-  const int lpr = 1 << lpr_log;
-  const int64_t chunk = (int64_t)blockIdx.x * (kThreads >> lpr_log) + (threadIdx.x >> lpr_log);
-  const int col = ((int)blockIdx.y * lpr + ((int)threadIdx.x & (lpr - 1))) * V;
-  if (chunk >= chunks || col >= a.dim) return;
+__global__ __launch_bounds__(kSumThreads) void embed_join_kernel(const EmbedGradArgs a, const SumShape sh) {
+  __shared__ float sum[kSumThreads * V];
   const uint32_t* __restrict__ keys = a.keys[(a.passes + 1) & 1];
   const uint32_t none = (uint32_t)a.num_rows;
-  const int64_t begin = chunk * kSumChunk, end = begin + kSumChunk;
-  if (end >= a.tokens) return;
+  const int64_t span = blockIdx.x, begin = span * sh.span, end = begin + sh.span;   // one more span follows
   const uint32_t row = keys[end - 1];
-  if (row == none || keys[end] != row) return;                                    // nothing goes on after this chunk
-  if (begin > 0 && keys[begin] == row && keys[begin - 1] == row) return;          // it began before this chunk
+  if (row == none || keys[end] != row) return;                               // nothing goes on after this span
+  if (begin > 0 && keys[begin] == row && keys[begin - 1] == row) return;     // it began before this span
+  const int lpr = 1 << sh.lpr_log, groups = kSumThreads >> sh.lpr_log, g = threadIdx.x >> sh.lpr_log;
+  const int col = ((int)blockIdx.y * lpr + ((int)threadIdx.x & (lpr - 1))) * V;
+  const bool mine = col < a.dim;
   float acc[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) acc[j] = a.part[(chunk * 2 + 1) * a.dim + col + j];
-  for (int64_t c = chunk + 1; c < chunks && keys[c * kSumChunk] == row; ++c) {
+  for (int j = 0; j < V; ++j) acc[j] = 0.f;
+  for (int64_t k = span + 1 + g; k < sh.spans && keys[k * sh.span] == row; k += groups) {
+    if (!mine) continue;
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += a.part[c * 2 * a.dim + col + j];
+    for (int j = 0; j < V; ++j) acc[j] += a.part[k * 2 * a.dim + col + j];
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[threadIdx.x * V + j] = acc[j];
+  __syncthreads();
+  if (g != 0 || !mine) return;
+#pragma unroll
+  for (int j = 0; j < V; ++j) acc[j] = a.part[(span * 2 + 1) * a.dim + col + j];
+  for (int k = 0; k < groups; ++k) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] += sum[(threadIdx.x + (k << sh.lpr_log)) * V + j];
   }
   write_row<V>(a, row, col, acc);
 }
-
-__global__ __launch_bounds__(kThreads) void fill_zero_kernel(void* p, int64_t bytes) {
-  typedef int quad __attribute__((ext_vector_type(4)));
-  const int64_t step = (int64_t)gridDim.x * kThreads, me = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t quads = (reinterpret_cast<uintptr_t>(p) & 15) == 0 ? bytes / 16 : 0;
-  for (int64_t i = me; i < quads; i += step) static_cast<quad*>(p)[i] = quad{0, 0, 0, 0};
-  for (int64_t i = quads * 8 + me; i < bytes / 2; i += step) static_cast<uint16_t*>(p)[i] = 0;
-}
-
 
 int lanes_log(int32_t dim, int v) {
   int l = 0;
   while (l < 6 && (int64_t)v << l < dim) ++l;
   return l;
+}
+
+// Chunks of at most kSumMaxChunk tokens, shorter ones where that leaves fewer than a thousand workgroups.
+SumShape sum_shape(int64_t tokens, int lpr_log) {
+  SumShape sh{};
+  sh.lpr_log = lpr_log;
+  const int64_t groups = kSumThreads >> lpr_log;
+  sh.chunk = kSumMaxChunk;
+  while (sh.chunk > 8 && tokens < 1024 * groups * sh.chunk) sh.chunk /= 2;
+  sh.span = groups * sh.chunk;
+  sh.spans = (tokens + sh.span - 1) / sh.span;
+  return sh;
+}
+
+// The most spans that a call can have, whatever pieces its rows allow.
+int64_t part_spans(int64_t tokens, int32_t dim) {
+  int64_t most = 0;
+  for (int v = 1; v <= 8; v *= 2) most = std::max(most, sum_shape(tokens, lanes_log(dim, v)).spans);
+  return most;
 }
 
 template <typename TIN, typename TOUT, int V>
@@ -300,13 +546,12 @@ hipError_t forward_by_out(const EmbedArgs& a, hipStream_t s) {
 
 template <typename TIN, int V>
 hipError_t run_sums(const EmbedGradArgs& a, hipStream_t s) {
-  const int l = lanes_log(a.dim, V);
-  const int64_t chunks = (a.tokens + kSumChunk - 1) / kSumChunk, groups = kThreads >> l;
-  const dim3 grid((unsigned)((chunks + groups - 1) / groups), (unsigned)((a.dim + (V << l) - 1) / (V << l)));
-  embed_sum_kernel<TIN, V><<<grid, kThreads, 0, s>>>(a, l, chunks);
+  const SumShape sh = sum_shape(a.tokens, lanes_log(a.dim, V));
+  const unsigned columns = (unsigned)((a.dim + (V << sh.lpr_log) - 1) / (V << sh.lpr_log));
+  embed_sum_kernel<TIN, V><<<dim3((unsigned)sh.spans, columns), kSumThreads, 0, s>>>(a, sh);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  embed_join_kernel<V><<<grid, kThreads, 0, s>>>(a, l, chunks);
+  if (e != hipSuccess || sh.spans == 1) return e;
+  embed_join_kernel<V><<<dim3((unsigned)sh.spans - 1, columns), kSumThreads, 0, s>>>(a, sh);
   return hipGetLastError();
 }
 
@@ -336,8 +581,8 @@ EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens)
   while (key_bits < 32 && (num_rows >> key_bits) != 0) ++key_bits;   // keys are 0 .. num_rows
   L.passes = (key_bits + kSortMaxBits - 1) / kSortMaxBits;
   L.bits = (key_bits + L.passes - 1) / L.passes;
-  L.tiles = (tokens + kSortTile - 1) / kSortTile;
-  L.chunks = (tokens + kSumChunk - 1) / kSumChunk;
+  const int64_t tile = kSortThreads * (tokens <= kSortFewTokens ? kSortFewItems : kSortManyItems);
+  L.tiles = tokens <= kSortOneThreads * kSortOneItems ? 1 : (tokens + tile - 1) / tile;
   size_t off = 0;
   const auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -348,7 +593,7 @@ EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens)
   for (int k = 0; k < 2; ++k) L.toks[k] = take((size_t)tokens * 4);
   L.hist = take(((size_t)L.tiles << L.bits) * 4);
   L.total = take((size_t(1) << L.bits) * 4);
-  L.part = take((size_t)L.chunks * 2 * (size_t)dim * 4);
+  L.part = take((size_t)part_spans(tokens, dim) * 2 * (size_t)dim * 4);
   L.bytes = std::max<size_t>(off, 256);
   return L;
 }
@@ -360,21 +605,34 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t s) {
   return forward_by_out<bf16_t>(a, s);
 }
 
-hipError_t launch_embed_grad(const EmbedGradArgs& a, hipStream_t s) {
+hipError_t launch_embed_grad(const EmbedGradArgs& args, hipStream_t s) {
+  EmbedGradArgs a = args;
   const int64_t bytes = a.num_rows * a.dim * elem_size(a.grad_dtype);
+  // a workgroup that zeroes has some 64 KB of it
+  const auto zero_blocks = [&](int shares) { return std::min<int64_t>((bytes / shares + 65535) / 65536, 8192); };
   hipError_t e = hipSuccess;
-  if (bytes > 0) {
-    const int64_t blocks = std::min<int64_t>((bytes / 16 + kThreads) / kThreads, 8192);
-    fill_zero_kernel<<<dim3((unsigned)blocks), kThreads, 0, s>>>(a.grad, bytes);
+  if (a.tiles == 1 || a.tokens == 0) {
+    a.launches = 1;
+    sort_one_kernel<<<dim3((unsigned)(1 + zero_blocks(1))), kSortOneThreads, 0, s>>>(a);
     e = hipGetLastError();
-  }
-  if (a.tokens == 0) return e;
-  const int64_t tiles = (a.tokens + kSortTile - 1) / kSortTile;
-  for (int p = 0; p < a.passes && e == hipSuccess; ++p) {
-    sort_count_kernel<<<dim3((unsigned)tiles), kSortThreads, 0, s>>>(a, p);
-    sort_scan_kernel<<<dim3(1u << a.bits), 64, 0, s>>>(a, tiles);
-    sort_scatter_kernel<<<dim3((unsigned)tiles), kSortThreads, 0, s>>>(a, p);
-    e = hipGetLastError();
+    if (a.tokens == 0) return e;
+  } else {
+    a.launches = 3 * a.passes;
+    const int64_t zero = zero_blocks(a.launches);
+    const dim3 tiles((unsigned)(a.tiles + zero)), scan((unsigned)(((1 << a.bits) + 63) / 64 + zero));
+    const bool few = a.tokens <= kSortFewTokens;
+    for (int p = 0; p < a.passes && e == hipSuccess; ++p) {
+      if (few)
+        sort_count_kernel<kSortFewItems><<<tiles, kSortThreads, 0, s>>>(a, p);
+      else
+        sort_count_kernel<kSortManyItems><<<tiles, kSortThreads, 0, s>>>(a, p);
+      sort_scan_kernel<<<scan, 64 * kSortScanWaves, 0, s>>>(a, p);
+      if (few)
+        sort_scatter_kernel<kSortFewItems><<<tiles, kSortThreads, 0, s>>>(a, p);
+      else
+        sort_scatter_kernel<kSortManyItems><<<tiles, kSortThreads, 0, s>>>(a, p);
+      e = hipGetLastError();
+    }
   }
   if (e != hipSuccess) return e;
   if (a.dout_dtype == DPI_F32) return sums_by_piece<float>(a, s);

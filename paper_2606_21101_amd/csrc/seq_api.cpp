@@ -213,6 +213,7 @@ dpi_status dpi_embed_backward(const void* dout, int32_t dout_dtype, int64_t dout
     a.part = reinterpret_cast<float*>(ws + L.part);
     a.passes = L.passes;
     a.bits = L.bits;
+    a.tiles = L.tiles;
   }
   a.dout = dout;
   a.ids = ids;

@@ -23,10 +23,12 @@ struct EmbedArgs {
 // Tokens sorted by id for the gradient: least significant digit first, two
 // ping-pong pairs of key and token arrays.
 constexpr int kSortThreads = 256;
-constexpr int kSortItems = 16;                              // items per thread
-constexpr int kSortTile = kSortThreads * kSortItems;        // items per block
-constexpr int kSortMaxBits = 8;                             // bits of a digit
-constexpr int kSumChunk = 64;                               // sorted tokens summed by one group of lanes
+constexpr int kSortMaxBits = 10;                            // bits of a digit
+constexpr int kSortFewItems = 4, kSortManyItems = 16;       // items per thread ...
+constexpr int64_t kSortFewTokens = 1 << 19;                 // ... up to this many tokens, beyond
+constexpr int kSortOneThreads = 1024, kSortOneItems = 4;    // the workgroup that sorts a short list alone
+constexpr int kSumThreads = 256;
+constexpr int kSumMaxChunk = 32;                            // most sorted tokens that one group of lanes sums
 
 struct EmbedGradArgs {
   const void* dout;
@@ -39,15 +41,18 @@ struct EmbedGradArgs {
   // workspace
   uint32_t* keys[2];
   uint32_t* toks[2];
-  uint32_t* hist;      // [bins][tiles]
+  uint32_t* hist;      // [tiles][bins]
   uint32_t* total;     // [bins]
-  float* part;         // [chunks][2][dim]: a chunk's part of a row that began before it, of one that goes on after it
+  float* part;         // [spans][2][dim]: a workgroup's part of a row that began before its span of sorted tokens, and of
+                       // one that goes on after it
   int32_t passes, bits;
+  int64_t tiles;
+  int32_t launches;    // that take a share of the zero rows
 };
 
 struct EmbedGradLayout {
   int32_t passes, bits;
-  int64_t tiles, chunks;
+  int64_t tiles;       // 1: one workgroup sorts alone
   size_t keys[2], toks[2], hist, total, part, bytes;
 };
 EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens);
