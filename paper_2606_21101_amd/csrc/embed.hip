@@ -11,8 +11,11 @@
 // begins and ends in it; rows cut by chunk borders are joined in LDS, those cut
 // by span borders by a second kernel.  Every sum has a fixed order and there
 // are no float atomics, so the result does not depend on timing.  The rows
-// without tokens are zeroed by workgroups of the sort's launches, which leave
-// the memory idle otherwise.  The bound is HBM: dout read, the gradient written.
+// without tokens are zeroed by workgroups of the sort's later launches, which
+// leave the memory idle otherwise, from marks that its first pass sets (all rows
+// zeroed beside the sort, the touched ones to be written again by the sums: 379
+// us for 2.1 M tokens of 128 bf16 over 1 M rows).  The bound is HBM: dout read,
+// the gradient written.
 #include "elem.h"
 #include "seq_internal.h"
 #include "wave_scan.h"
@@ -67,16 +70,65 @@ __device__ __forceinline__ uint32_t key_of(const EmbedGradArgs& a, int64_t i, bo
   return pad || !inside ? (uint32_t)a.num_rows : (uint32_t)id;   // num_rows: after every row, in no row's sum
 }
 
-// Share `share` of a.launches of the gradient set to zero by `blocks` workgroups, of which this is `block`.
-__device__ __forceinline__ void zero_share(const EmbedGradArgs& a, int share, int64_t block, int64_t blocks) {
+// One row of `units` units, by the lanes of a group.
+template <typename U>
+__device__ __forceinline__ void zero_row(void* row, int units, int lane, int lanes) {
+  for (int i = lane; i < units; i += lanes) static_cast<U*>(row)[i] = U{};
+}
+
+// Share `share` of a.zero_shares of the gradient's rows set to zero by `blocks` workgroups, of which this is `block`;
+// MARKED: but those with tokens.
+template <bool MARKED>
+__device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, int share, int64_t block, int64_t blocks) {
   typedef int quad __attribute__((ext_vector_type(4)));
-  const int64_t bytes = a.num_rows * a.dim * (a.grad_dtype == DPI_F32 ? 4 : 2);
-  const int64_t step = blocks * blockDim.x, me = block * blockDim.x + threadIdx.x;
-  const int64_t quads = (reinterpret_cast<uintptr_t>(a.grad) & 15) == 0 ? bytes / 16 : 0;
-  const int64_t end = quads * (share + 1) / a.launches;
-  for (int64_t i = quads * share / a.launches + me; i < end; i += step) static_cast<quad*>(a.grad)[i] = quad{0, 0, 0, 0};
-  if (share == 0)   // what 16-byte stores cannot reach
-    for (int64_t i = quads * 8 + me; i < bytes / 2; i += step) static_cast<uint16_t*>(a.grad)[i] = 0;
+  const int64_t row_bytes = (int64_t)a.dim * (a.grad_dtype == DPI_F32 ? 4 : 2);
+  const uint32_t odd = (uint32_t)(reinterpret_cast<uintptr_t>(a.grad) | (uintptr_t)row_bytes);
+  const int unit = odd & 15 ? (odd & 3 ? 2 : 4) : 16, units = (int)(row_bytes / unit);
+  int lanes_log = 0;
+  while (lanes_log < 6 && (1 << lanes_log) < units) ++lanes_log;
+  const int lanes = 1 << lanes_log, lane = threadIdx.x & (lanes - 1);
+  const int64_t groups = blockDim.x >> lanes_log, end = a.num_rows * (share + 1) / a.zero_shares;
+  const int64_t step = blocks * groups;
+  for (int64_t r = a.num_rows * share / a.zero_shares + block * groups + (threadIdx.x >> lanes_log); r < end; r += 4 * step) {
+    bool held[4];   // four rows' marks in flight
+#pragma unroll
+    for (int u = 0; u < 4; ++u) held[u] = r + u * step >= end || (MARKED && a.touched[r + u * step]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (held[u]) continue;
+      char* row = static_cast<char*>(a.grad) + (r + u * step) * row_bytes;
+      if (unit == 16)
+        zero_row<quad>(row, units, lane, lanes);
+      else if (unit == 4)
+        zero_row<int>(row, units, lane, lanes);
+      else
+        zero_row<int16_t>(row, units, lane, lanes);
+    }
+  }
+}
+
+// What the workgroups beside the sort's own do in launch `step` (count, scan, scatter) of a pass: clear the marks in the
+// first launch; the first pass's scatter sets them; every later launch zeroes a share of the rows, with the marks once
+// they are set.  A sort of one pass, of few rows, zeroes them all in the first launch.
+__device__ __forceinline__ void beside_sort(const EmbedGradArgs& a, int pass, int step, int64_t block, int64_t blocks) {
+  if (a.passes == 1) {
+    if (step == 0) zero_rows<false>(a, 0, block, blocks);
+  } else if (pass > 0) {
+    zero_rows<true>(a, 3 * pass + step - 1, block, blocks);
+  } else if (step > 0) {
+    zero_rows<false>(a, step - 1, block, blocks);
+  } else {
+    for (int64_t i = block * blockDim.x + threadIdx.x; i < (a.num_rows + 15) / 16; i += blocks * blockDim.x)
+      reinterpret_cast<int4*>(a.touched)[i] = int4{0, 0, 0, 0};
+  }
+}
+
+// A tile of the sort: workgroups go to the 8 XCDs in turn, and the tiles of an XCD are neighbours, so that the few items
+// that each of them has of a digit, which lie side by side in the output, fill cache lines of one L2.
+__device__ __forceinline__ int64_t tile_of(const EmbedGradArgs& a) {
+  const int64_t per = (a.tiles + 7) >> 3, x = blockIdx.x & 7, i = blockIdx.x >> 3;
+  const int64_t whole = a.tiles & 7;   // XCDs with `per` tiles when they do not divide evenly
+  return whole == 0 || x < whole ? x * per + i : whole * per + (x - whole) * (per - 1) + i;
 }
 
 // Exclusive prefix over the workgroup of one value a thread; *total: their sum.  sums: a word a wave, free to use.
@@ -116,25 +168,25 @@ template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const EmbedGradArgs a, int pass) {
   __shared__ uint32_t count[1 << kSortMaxBits];
   if (blockIdx.x >= a.tiles) {
-    zero_share(a, 3 * pass, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    beside_sort(a, pass, 0, blockIdx.x - a.tiles, gridDim.x - a.tiles);
     return;
   }
   const int bins = 1 << a.bits, shift = pass * a.bits;
-  const int64_t base = (int64_t)blockIdx.x * kSortThreads * ITEMS;
+  const int64_t tile = tile_of(a), base = tile * kSortThreads * ITEMS;
   for (int b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
-  const uint32_t* __restrict__ keys = a.keys[(pass + 1) & 1];
+  const uint2* __restrict__ pairs = a.pairs[(pass + 1) & 1];
   uint32_t key[ITEMS];
 #pragma unroll
   for (int u = 0; u < ITEMS; ++u) {
     const int64_t i = base + u * kSortThreads + threadIdx.x;
-    key[u] = i < a.tokens ? (pass == 0 ? key_of(a, i, true) : keys[i]) : 0;
+    key[u] = i < a.tokens ? (pass == 0 ? key_of(a, i, true) : pairs[i].x) : 0;
   }
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < ITEMS; ++u)
     if (base + u * kSortThreads + threadIdx.x < a.tokens) atomicAdd(&count[(key[u] >> shift) & (bins - 1)], 1u);
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += kSortThreads) a.hist[((int64_t)blockIdx.x << a.bits) + b] = count[b];
+  for (int b = threadIdx.x; b < bins; b += kSortThreads) a.hist[(tile << a.bits) + b] = count[b];
 }
 
 // The tiles' counts of 64 digits to their exclusive prefixes over the tiles, and the digits' totals: a lane a digit, the
@@ -145,7 +197,7 @@ __global__ __launch_bounds__(64 * kSortScanWaves) void sort_scan_kernel(const Em
   __shared__ uint32_t sums[kSortScanWaves][64];
   const int bins = 1 << a.bits, groups = (bins + 63) / 64;
   if ((int)blockIdx.x >= groups) {
-    zero_share(a, 3 * pass + 1, blockIdx.x - groups, gridDim.x - groups);
+    beside_sort(a, pass, 1, blockIdx.x - groups, gridDim.x - groups);
     return;
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -186,23 +238,19 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedG
   __shared__ uint32_t next[kWaves][1 << kSortMaxBits];
   __shared__ uint32_t sums[kWaves];
   if (blockIdx.x >= a.tiles) {
-    zero_share(a, 3 * pass + 2, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    beside_sort(a, pass, 2, blockIdx.x - a.tiles, gridDim.x - a.tiles);
     return;
   }
   const int bins = 1 << a.bits, shift = pass * a.bits;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t base = ((int64_t)blockIdx.x * kWaves + wave) * 64 * ITEMS;   // a wave's items are consecutive
-  uint32_t key[ITEMS], tok[ITEMS];
-  const uint32_t* __restrict__ keys = a.keys[(pass + 1) & 1];
-  const uint32_t* __restrict__ toks = a.toks[(pass + 1) & 1];
+  const int64_t tile = tile_of(a), base = (tile * kWaves + wave) * 64 * ITEMS;   // a wave's items are consecutive
+  uint2 item[ITEMS];
+  const uint2* __restrict__ pairs = a.pairs[(pass + 1) & 1];
 #pragma unroll
   for (int u = 0; u < ITEMS; ++u) {
     const int64_t i = base + u * 64 + lane;
-    key[u] = tok[u] = 0;
-    if (i < a.tokens) {
-      key[u] = pass == 0 ? key_of(a, i, false) : keys[i];
-      tok[u] = pass == 0 ? (uint32_t)i : toks[i];
-    }
+    item[u] = uint2{0, 0};
+    if (i < a.tokens) item[u] = pass == 0 ? uint2{key_of(a, i, false), (uint32_t)i} : pairs[i];
   }
   // kEach neighbouring digits a thread: where they start, and this tile's part of them
   uint32_t total[kEach], mine[kEach], sum = 0;
@@ -210,7 +258,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedG
   for (int j = 0; j < kEach; ++j) {
     const int b = threadIdx.x * kEach + j;
     total[j] = b < bins ? a.total[b] : 0;
-    mine[j] = b < bins ? a.hist[((int64_t)blockIdx.x << a.bits) + b] : 0;
+    mine[j] = b < bins ? a.hist[(tile << a.bits) + b] : 0;
     sum += total[j];
   }
   for (int b = threadIdx.x; b < bins; b += kSortThreads) {
@@ -221,7 +269,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedG
   uint32_t start = block_prefix<kSortThreads>(sum, sums, &all);   // its barrier also ends the clearing
 #pragma unroll
   for (int u = 0; u < ITEMS; ++u)
-    if (base + u * 64 + lane < a.tokens) atomicAdd(&next[wave][(key[u] >> shift) & (bins - 1)], 1u);
+    if (base + u * 64 + lane < a.tokens) atomicAdd(&next[wave][(item[u].x >> shift) & (bins - 1)], 1u);
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
@@ -238,16 +286,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedG
     start += total[j];
   }
   __syncthreads();
-  uint32_t* __restrict__ keys_out = a.keys[pass & 1];
-  uint32_t* __restrict__ toks_out = a.toks[pass & 1];
+  uint2* __restrict__ out = a.pairs[pass & 1];
+  const bool mark = pass == 0 && a.passes > 1;
 #pragma unroll
   for (int u = 0; u < ITEMS; ++u) {
     const bool live = base + u * 64 + lane < a.tokens;
-    const uint32_t at = place_of_digit((key[u] >> shift) & (bins - 1), live, a.bits, lane, next[wave]);
-    if (live) {
-      keys_out[at] = key[u];
-      toks_out[at] = tok[u];
-    }
+    const uint32_t at = place_of_digit((item[u].x >> shift) & (bins - 1), live, a.bits, lane, next[wave]);
+    if (live) out[at] = item[u];
+    if (live && mark && item[u].x < (uint32_t)a.num_rows) a.touched[item[u].x] = 1;   // the same by whoever writes it
   }
 }
 
@@ -260,7 +306,7 @@ __global__ __launch_bounds__(kSortOneThreads) void sort_one_kernel(const EmbedGr
   __shared__ uint32_t lkey[kTile], ltok[kTile];
   __shared__ uint32_t sums[kWaves];
   if (blockIdx.x > 0) {
-    zero_share(a, 0, blockIdx.x - 1, gridDim.x - 1);
+    zero_rows<false>(a, 0, blockIdx.x - 1, gridDim.x - 1);
     return;
   }
   const int bins = 1 << a.bits, n = (int)a.tokens;
@@ -318,15 +364,11 @@ __global__ __launch_bounds__(kSortOneThreads) void sort_one_kernel(const EmbedGr
       }
     }
   }
-  uint32_t* __restrict__ keys_out = a.keys[(a.passes + 1) & 1];
-  uint32_t* __restrict__ toks_out = a.toks[(a.passes + 1) & 1];
+  uint2* __restrict__ out = a.pairs[(a.passes + 1) & 1];
 #pragma unroll
   for (int u = 0; u < kSortOneItems; ++u) {
     const int i = base + u * 64 + lane;
-    if (i < n) {
-      keys_out[i] = key[u];
-      toks_out[i] = tok[u];
-    }
+    if (i < n) out[i] = uint2{key[u], tok[u]};
   }
 }
 
@@ -362,8 +404,7 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradA
   __shared__ uint32_t state[kSumThreads];                          // of each group
   const int lpr = 1 << sh.lpr_log, groups = kSumThreads >> sh.lpr_log, g = threadIdx.x >> sh.lpr_log;
   const int col = ((int)blockIdx.y * lpr + ((int)threadIdx.x & (lpr - 1))) * V;
-  const uint32_t* __restrict__ keys = a.keys[(a.passes + 1) & 1];
-  const uint32_t* __restrict__ toks = a.toks[(a.passes + 1) & 1];
+  const uint2* __restrict__ pairs = a.pairs[(a.passes + 1) & 1];
   const TIN* __restrict__ dout = static_cast<const TIN*>(a.dout);
   const uint32_t none = (uint32_t)a.num_rows;
   const int64_t begin = (int64_t)blockIdx.x * sh.span + g * sh.chunk, end = min(begin + sh.chunk, a.tokens);
@@ -373,17 +414,18 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradA
   for (int j = 0; j < V; ++j) acc[j] = 0.f;
   uint32_t how = 0, row = none, last_row = none;
   if (begin < end) {
-    row = keys[begin];
-    bool cut = row != none && begin > 0 && keys[begin - 1] == row;
+    row = pairs[begin].x;
+    bool cut = row != none && begin > 0 && pairs[begin - 1].x == row;
     if (cut) how |= kRowCut;
     for (int64_t i0 = begin; i0 < end && row != none; i0 += 8) {
       uint32_t key[9], tok[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        tok[u] = toks[min(i0 + u, a.tokens - 1)];
-        key[u] = keys[min(i0 + u, a.tokens - 1)];
+        const uint2 item = pairs[min(i0 + u, a.tokens - 1)];
+        key[u] = item.x;
+        tok[u] = item.y;
       }
-      key[8] = i0 + 8 < a.tokens ? keys[i0 + 8] : none;
+      key[8] = i0 + 8 < a.tokens ? pairs[i0 + 8].x : none;
       Elems<TIN, V> e[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u)
@@ -451,39 +493,101 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradA
   }
 }
 
-// The rows cut by span borders: a workgroup for the span in which one begins, its groups of lanes taking turns at the
-// spans after it.
+// The rows cut by span borders.  A wave for the span in which one begins adds the parts of up to 7 spans after it, its
+// groups of lanes taking turns; a row that goes on further is the whole workgroup's.  (A workgroup for every span took 28
+// us for 4,096 spans: each waits for memory a few times, and they did not all fit at once.)
+constexpr int kJoinWaves = kSumThreads / 64, kJoinNear = 8;
+
 template <int V>
 __global__ __launch_bounds__(kSumThreads) void embed_join_kernel(const EmbedGradArgs a, const SumShape sh) {
   __shared__ float sum[kSumThreads * V];
-  const uint32_t* __restrict__ keys = a.keys[(a.passes + 1) & 1];
+  __shared__ int64_t far[kJoinWaves];   // the waves' spans whose row goes far, or -1
+  const uint2* __restrict__ pairs = a.pairs[(a.passes + 1) & 1];
   const uint32_t none = (uint32_t)a.num_rows;
-  const int64_t span = blockIdx.x, begin = span * sh.span, end = begin + sh.span;   // one more span follows
-  const uint32_t row = keys[end - 1];
-  if (row == none || keys[end] != row) return;                               // nothing goes on after this span
-  if (begin > 0 && keys[begin] == row && keys[begin - 1] == row) return;     // it began before this span
-  const int lpr = 1 << sh.lpr_log, groups = kSumThreads >> sh.lpr_log, g = threadIdx.x >> sh.lpr_log;
-  const int col = ((int)blockIdx.y * lpr + ((int)threadIdx.x & (lpr - 1))) * V;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lpr = 1 << sh.lpr_log, col = ((int)blockIdx.y * lpr + (lane & (lpr - 1))) * V;
   const bool mine = col < a.dim;
-  float acc[V];
+  // how many of `window` spans from k0 on begin with the row, a lane each
+  const auto follow = [&](uint32_t row, int64_t k0, int window, uint32_t start) {
+    const uint64_t same = __ballot(k0 + lane < sh.spans && lane < window && start == row);
+    return ~same ? __builtin_ctzll(~same) : 64;
+  };
+  const auto start_of = [&](int64_t k0, int window) { return pairs[min(k0 + min(lane, window - 1), sh.spans - 1) * sh.span].x; };
+  const auto part_of = [&](int64_t k, int which, bool use, float* v) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) acc[j] = 0.f;
-  for (int64_t k = span + 1 + g; k < sh.spans && keys[k * sh.span] == row; k += groups) {
-    if (!mine) continue;
+    for (int j = 0; j < V; ++j) v[j] = use && mine ? a.part[(k * 2 + which) * a.dim + col + j] : 0.f;
+  };
+  {
+    const int64_t span = (int64_t)blockIdx.x * kJoinWaves + wave;
+    int64_t goes_far = -1;
+    if (span + 1 < sh.spans) {
+      const int64_t begin = span * sh.span, end = begin + sh.span;
+      const uint32_t row = pairs[end - 1].x, first_row = pairs[begin].x, before = pairs[max(begin - 1, (int64_t)0)].x;
+      const bool goes_on = row != none && pairs[end].x == row;
+      if (goes_on && !(begin > 0 && first_row == row && before == row)) {   // a row that begins in this span
+        const int many = follow(row, span + 1, kJoinNear, start_of(span + 1, kJoinNear));
+        if (many == kJoinNear) {
+          goes_far = span;
+        } else {
+          const int groups = 64 >> sh.lpr_log, g = lane >> sh.lpr_log;
+          float acc[V], v[V];
+          part_of(span, 1, g == 0, acc);
+          for (int i = g; i < many; i += groups) {
+            part_of(span + 1 + i, 0, true, v);
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += a.part[k * 2 * a.dim + col + j];
+            for (int j = 0; j < V; ++j) acc[j] += v[j];
+          }
+          for (int d = lpr; d < 64; d <<= 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] += __shfl_xor(acc[j], d, 64);
+          }
+          if (g == 0 && mine) write_row<V>(a, row, col, acc);
+        }
+      }
+    }
+    if (lane == 0) far[wave] = goes_far;
   }
-#pragma unroll
-  for (int j = 0; j < V; ++j) sum[threadIdx.x * V + j] = acc[j];
   __syncthreads();
-  if (g != 0 || !mine) return;
+  for (int w = 0; w < kJoinWaves; ++w) {
+    const int64_t span = far[w];
+    if (span < 0) continue;
+    const int groups = kSumThreads >> sh.lpr_log, g = threadIdx.x >> sh.lpr_log;
+    const uint32_t row = pairs[(span + 1) * sh.span - 1].x;
+    float acc[V];
+    part_of(span, 1, g == 0, acc);
+    int64_t k0 = span + 1;
+    int many = follow(row, k0, 64, start_of(k0, 64));
+    for (;;) {   // 64 spans at a time, four of a group's in flight, and the next ones' starts
+      const bool more = many == 64;
+      const uint32_t start = more ? start_of(k0 + 64, 64) : 0;
+      for (int i0 = g; i0 < many; i0 += 4 * groups) {
+        float v[4][V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) acc[j] = a.part[(span * 2 + 1) * a.dim + col + j];
-  for (int k = 0; k < groups; ++k) {
+        for (int u = 0; u < 4; ++u) part_of(k0 + i0 + u * groups, 0, i0 + u * groups < many, v[u]);
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += sum[(threadIdx.x + (k << sh.lpr_log)) * V + j];
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] += v[u][j];
+        }
+      }
+      if (!more) break;
+      k0 += 64;
+      many = follow(row, k0, 64, start);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[threadIdx.x * V + j] = acc[j];
+    __syncthreads();
+    if (g == 0 && mine) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) acc[j] = 0.f;
+      for (int k = 0; k < groups; ++k) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += sum[(threadIdx.x + (k << sh.lpr_log)) * V + j];
+      }
+      write_row<V>(a, row, col, acc);
+    }
+    __syncthreads();
   }
-  write_row<V>(a, row, col, acc);
 }
 
 int lanes_log(int32_t dim, int v) {
@@ -551,7 +655,7 @@ hipError_t run_sums(const EmbedGradArgs& a, hipStream_t s) {
   embed_sum_kernel<TIN, V><<<dim3((unsigned)sh.spans, columns), kSumThreads, 0, s>>>(a, sh);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sh.spans == 1) return e;
-  embed_join_kernel<V><<<dim3((unsigned)sh.spans - 1, columns), kSumThreads, 0, s>>>(a, sh);
+  embed_join_kernel<V><<<dim3((unsigned)((sh.spans - 1 + kJoinWaves - 1) / kJoinWaves), columns), kSumThreads, 0, s>>>(a, sh);
   return hipGetLastError();
 }
 
@@ -589,8 +693,8 @@ EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens)
     off = (off + bytes + 255) & ~size_t(255);
     return at;
   };
-  for (int k = 0; k < 2; ++k) L.keys[k] = take((size_t)tokens * 4);
-  for (int k = 0; k < 2; ++k) L.toks[k] = take((size_t)tokens * 4);
+  for (int k = 0; k < 2; ++k) L.pairs[k] = take((size_t)tokens * 8);
+  L.touched = take((size_t)num_rows);
   L.hist = take(((size_t)L.tiles << L.bits) * 4);
   L.total = take((size_t(1) << L.bits) * 4);
   L.part = take((size_t)part_spans(tokens, dim) * 2 * (size_t)dim * 4);
@@ -608,18 +712,18 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t s) {
 hipError_t launch_embed_grad(const EmbedGradArgs& args, hipStream_t s) {
   EmbedGradArgs a = args;
   const int64_t bytes = a.num_rows * a.dim * elem_size(a.grad_dtype);
-  // a workgroup that zeroes has some 64 KB of it
-  const auto zero_blocks = [&](int shares) { return std::min<int64_t>((bytes / shares + 65535) / 65536, 8192); };
+  // a workgroup that zeroes has some 16 KB of it
+  const auto zero_blocks = [&](int shares) { return std::min<int64_t>((bytes / shares + 16383) / 16384, 4096); };
   hipError_t e = hipSuccess;
   if (a.tiles == 1 || a.tokens == 0) {
-    a.launches = 1;
+    a.zero_shares = 1;
     sort_one_kernel<<<dim3((unsigned)(1 + zero_blocks(1))), kSortOneThreads, 0, s>>>(a);
     e = hipGetLastError();
     if (a.tokens == 0) return e;
   } else {
-    a.launches = 3 * a.passes;
-    const int64_t zero = zero_blocks(a.launches);
-    const dim3 tiles((unsigned)(a.tiles + zero)), scan((unsigned)(((1 << a.bits) + 63) / 64 + zero));
+    a.zero_shares = a.passes == 1 ? 1 : 3 * a.passes - 1;
+    const int64_t zero = zero_blocks(a.zero_shares);
+    const dim3 tiles((unsigned)(a.tiles + zero)), scan((unsigned)(((1 << a.bits) + 63) / 64 + (zero + 3) / 4));
     const bool few = a.tokens <= kSortFewTokens;
     for (int p = 0; p < a.passes && e == hipSuccess; ++p) {
       if (few)

@@ -204,10 +204,8 @@ dpi_status dpi_embed_backward(const void* dout, int32_t dout_dtype, int64_t dout
     const EmbedGradLayout L = embed_grad_layout(num_rows, dim, num_tokens);
     DPI_TRY(check_workspace(workspace, workspace_bytes, L.bytes));
     char* ws = static_cast<char*>(workspace);
-    for (int k = 0; k < 2; ++k) {
-      a.keys[k] = reinterpret_cast<uint32_t*>(ws + L.keys[k]);
-      a.toks[k] = reinterpret_cast<uint32_t*>(ws + L.toks[k]);
-    }
+    for (int k = 0; k < 2; ++k) a.pairs[k] = reinterpret_cast<uint2*>(ws + L.pairs[k]);
+    a.touched = reinterpret_cast<uint8_t*>(ws + L.touched);
     a.hist = reinterpret_cast<uint32_t*>(ws + L.hist);
     a.total = reinterpret_cast<uint32_t*>(ws + L.total);
     a.part = reinterpret_cast<float*>(ws + L.part);

@@ -21,7 +21,7 @@ struct EmbedArgs {
 };
 
 // Tokens sorted by id for the gradient: least significant digit first, two
-// ping-pong pairs of key and token arrays.
+// ping-pong arrays of (key, token) pairs.
 constexpr int kSortThreads = 256;
 constexpr int kSortMaxBits = 10;                            // bits of a digit
 constexpr int kSortFewItems = 4, kSortManyItems = 16;       // items per thread ...
@@ -39,21 +39,21 @@ struct EmbedGradArgs {
   int32_t dim, dout_dtype, grad_dtype, padding_id;
   float scale;
   // workspace
-  uint32_t* keys[2];
-  uint32_t* toks[2];
+  uint2* pairs[2];     // key (id), token
+  uint8_t* touched;    // [num_rows]: 1 where a row has tokens
   uint32_t* hist;      // [tiles][bins]
   uint32_t* total;     // [bins]
   float* part;         // [spans][2][dim]: a workgroup's part of a row that began before its span of sorted tokens, and of
                        // one that goes on after it
   int32_t passes, bits;
   int64_t tiles;
-  int32_t launches;    // that take a share of the zero rows
+  int32_t zero_shares;   // launches that zero rows
 };
 
 struct EmbedGradLayout {
   int32_t passes, bits;
   int64_t tiles;       // 1: one workgroup sorts alone
-  size_t keys[2], toks[2], hist, total, part, bytes;
+  size_t pairs[2], touched, hist, total, part, bytes;
 };
 EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens);
 
