@@ -57,6 +57,22 @@ __device__ __forceinline__ void store_elems(T* p, const float* v, int have) {
   }
 }
 
+// The same, all V there and aligned, past the caches' order of use: rows that nothing reads again soon.
+template <typename T, int V>
+__device__ __forceinline__ Elems<T, V> load_once(const T* p) {
+  Elems<T, V> e;
+  e.raw = __builtin_nontemporal_load(reinterpret_cast<const typename Raw<T, V>::type*>(p));
+  return e;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_once(T* p, const float* v) {
+  typename Raw<T, V>::plain r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) r[i] = (T)v[i];
+  __builtin_nontemporal_store(r, reinterpret_cast<typename Raw<T, V>::type*>(p));
+}
+
 }  // namespace
 
 inline int elem_size(int32_t dtype) { return dtype == DPI_F32 ? 4 : 2; }

@@ -15,7 +15,8 @@
 // leave the memory idle otherwise, from marks that its first pass sets (all rows
 // zeroed beside the sort, the touched ones to be written again by the sums: 379
 // us for 2.1 M tokens of 128 bf16 over 1 M rows).  The bound is HBM: dout read,
-// the gradient written.
+// the gradient written, both past the caches (the sums of that case: 194 us
+// through them, 157 past them, 4.5 TB/s).
 #include "elem.h"
 #include "seq_internal.h"
 #include "wave_scan.h"
@@ -73,7 +74,7 @@ __device__ __forceinline__ uint32_t key_of(const EmbedGradArgs& a, int64_t i, bo
 // One row of `units` units, by the lanes of a group.
 template <typename U>
 __device__ __forceinline__ void zero_row(void* row, int units, int lane, int lanes) {
-  for (int i = lane; i < units; i += lanes) static_cast<U*>(row)[i] = U{};
+  for (int i = lane; i < units; i += lanes) __builtin_nontemporal_store(U{}, static_cast<U*>(row) + i);
 }
 
 // Share `share` of a.zero_shares of the gradient's rows set to zero by `blocks` workgroups, of which this is `block`;
@@ -380,11 +381,11 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs& a, uint32_t row, 
   for (int j = 0; j < V; ++j) v[j] = a.scale * acc[j];
   const int64_t at = (int64_t)row * a.dim + col;
   if (a.grad_dtype == DPI_F32)
-    store_elems<true, float, V>(static_cast<float*>(a.grad) + at, v, V);
+    store_once<float, V>(static_cast<float*>(a.grad) + at, v);
   else if (a.grad_dtype == DPI_F16)
-    store_elems<true, f16_t, V>(static_cast<f16_t*>(a.grad) + at, v, V);
+    store_once<f16_t, V>(static_cast<f16_t*>(a.grad) + at, v);
   else
-    store_elems<true, bf16_t, V>(static_cast<bf16_t*>(a.grad) + at, v, V);
+    store_once<bf16_t, V>(static_cast<bf16_t*>(a.grad) + at, v);
 }
 
 // How a launch covers the sorted tokens: groups of 2^lpr_log lanes take `chunk` of them each, a workgroup's a span.
@@ -429,7 +430,7 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradA
       Elems<TIN, V> e[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (mine && i0 + u < end && key[u] != none) e[u] = load_elems<true, TIN, V>(dout + (int64_t)tok[u] * a.dout_stride + col, V);
+        if (mine && i0 + u < end && key[u] != none) e[u] = load_once<TIN, V>(dout + (int64_t)tok[u] * a.dout_stride + col);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int64_t i = i0 + u;
