@@ -3,7 +3,7 @@
 //   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
 //   p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
 //
-// A workgroup takes kAdamChunk elements of one tensor (its row of the chunk
+// A workgroup takes a chunk of one tensor's elements (its row of the chunk
 // table says which), a wave 256 elements at a time, a lane 4 neighbours.  The
 // bound is HBM: every array is read and written once.
 //
@@ -17,6 +17,7 @@
 // give equal bits.
 #include "elem.h"
 #include "seq_internal.h"
+#include "wave_scan.h"
 
 namespace dpi {
 namespace {
@@ -33,39 +34,44 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-template <typename T>
+// ONCE: the tensors do not fit the caches, so nothing of them is read from there again.
+template <bool ONCE, typename T>
 __device__ __forceinline__ void get4(const void* p, int64_t i, int have, bool wide, float* v) {
   const T* q = static_cast<const T*>(p) + i;
-  const Elems<T, 4> e = wide ? load_elems<true, T, 4>(q, have) : load_elems<false, T, 4>(q, have);
+  const Elems<T, 4> e = !wide ? load_elems<false, T, 4>(q, have) : ONCE ? load_once<T, 4>(q) : load_elems<true, T, 4>(q, have);
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = e[j];
 }
 
+template <bool ONCE>
 __device__ __forceinline__ void get4(int32_t dtype, const void* p, int64_t i, int have, bool wide, float* v) {
   if (dtype == DPI_F32)
-    get4<float>(p, i, have, wide, v);
+    get4<ONCE, float>(p, i, have, wide, v);
   else if (dtype == DPI_F16)
-    get4<f16_t>(p, i, have, wide, v);
+    get4<ONCE, f16_t>(p, i, have, wide, v);
   else
-    get4<bf16_t>(p, i, have, wide, v);
+    get4<ONCE, bf16_t>(p, i, have, wide, v);
 }
 
-template <typename T>
+template <bool ONCE, typename T>
 __device__ __forceinline__ void put4(void* p, int64_t i, int have, bool wide, const float* v) {
   T* q = static_cast<T*>(p) + i;
-  if (wide)
-    store_elems<true, T, 4>(q, v, have);
-  else
+  if (!wide)
     store_elems<false, T, 4>(q, v, have);
+  else if (ONCE)
+    store_once<T, 4>(q, v);
+  else
+    store_elems<true, T, 4>(q, v, have);
 }
 
+template <bool ONCE>
 __device__ __forceinline__ void put4(int32_t dtype, void* p, int64_t i, int have, bool wide, const float* v) {
   if (dtype == DPI_F32)
-    put4<float>(p, i, have, wide, v);
+    put4<ONCE, float>(p, i, have, wide, v);
   else if (dtype == DPI_F16)
-    put4<f16_t>(p, i, have, wide, v);
+    put4<ONCE, f16_t>(p, i, have, wide, v);
   else
-    put4<bf16_t>(p, i, have, wide, v);
+    put4<ONCE, bf16_t>(p, i, have, wide, v);
 }
 
 __device__ __forceinline__ void get4_codes(const void* p, int64_t i, int have, bool wide, float scale, float* v) {
@@ -81,6 +87,17 @@ __device__ __forceinline__ void get4_codes(const void* p, int64_t i, int have, b
   v[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale;
   v[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale;
   v[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * scale;
+}
+
+// The largest of the wave's values: the scan's steps with a maximum, whose identity the moved-in zeros are.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, dpp_or_zero<0x111, 0xf>(x));
+  x = max(x, dpp_or_zero<0x112, 0xf>(x));
+  x = max(x, dpp_or_zero<0x114, 0xf>(x));
+  x = max(x, dpp_or_zero<0x118, 0xf>(x));
+  x = max(x, dpp_or_zero<0x142, 0xa>(x));
+  x = max(x, dpp_or_zero<0x143, 0xc>(x));
+  return __builtin_amdgcn_readlane(x, 63);
 }
 
 // |x| / scale, at most 448, to an e4m3 code: rnd (20 bits) is added below the
@@ -99,11 +116,10 @@ __device__ __forceinline__ void put4_codes(void* p, float* scale, int64_t i, int
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+  top = wave_max(top);
   const float amax = __uint_as_float(top);
-  const bool none = amax <= 0x1p-100f;   // 448 / amax would leave the range: held as zeros
-  const float inv = none ? 0.f : 448.f / amax;
+  const bool none = amax <= 0x1p-100f;   // its reciprocal would near the range's end: held as zeros
+  const float inv = none ? 0.f : (1.f / amax) * 448.f;
   uint32_t w = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -123,7 +139,7 @@ __device__ __forceinline__ void put4_codes(void* p, float* scale, int64_t i, int
         if (j < have) q[j] = (uint8_t)(w >> (8 * j));
     }
   }
-  if ((threadIdx.x & 63) == 0) *scale = none ? 0.f : amax / 448.f;
+  if ((threadIdx.x & 63) == 0) *scale = none ? 0.f : amax * (1.f / 448.f);
 }
 
 __device__ __forceinline__ bool aligned_to(const void* p, int bytes) {
@@ -132,7 +148,7 @@ __device__ __forceinline__ bool aligned_to(const void* p, int bytes) {
 
 __device__ __forceinline__ int size_of(int32_t dtype) { return dtype == DPI_F32 ? 4 : 2; }
 
-template <bool BITS8>
+template <bool BITS8, bool ONCE>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
 #pragma clang fp contract(off)
   const AdamChunk c = a.chunks[a.first_chunk + blockIdx.x];
@@ -143,8 +159,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
   const uint32_t key = mix(a.seed + (uint32_t)c.tensor * 0xC2B2AE35u);
   const bool whole = aligned_to(t.param, 4 * size_of(t.param_dtype)) && aligned_to(grad, 4 * size_of(t.grad_dtype)) &&
                      aligned_to(t.master, 16) && aligned_to(t.m, BITS8 ? 4 : 16) && aligned_to(t.v, BITS8 ? 4 : 16);
-  for (int b = wave; b < kAdamChunk / kAdamBlock; b += kWaves) {
-    const int64_t block = (int64_t)c.chunk * (kAdamChunk / kAdamBlock) + b;
+  const int blocks = a.chunk / kAdamBlock;
+  for (int b = wave; b < blocks; b += kWaves) {
+    const int64_t block = (int64_t)c.chunk * blocks + b;
     if (block * kAdamBlock >= t.count) return;   // the same for the whole wave
     const int64_t i = block * kAdamBlock + lane * 4;
     const int have = (int)min((int64_t)4, t.count - i);   // elements of this lane: 0 or less past the end
@@ -153,17 +170,17 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) g[j] = m[j] = v[j] = p[j] = 0.f;
     if (have > 0) {
-      get4(t.grad_dtype, grad, i, have, wide, g);
+      get4<ONCE>(t.grad_dtype, grad, i, have, wide, g);
       if (t.master)
-        get4<float>(t.master, i, have, wide, p);
+        get4<ONCE, float>(t.master, i, have, wide, p);
       else
-        get4(t.param_dtype, t.param, i, have, wide, p);
+        get4<ONCE>(t.param_dtype, t.param, i, have, wide, p);
       if constexpr (BITS8) {
         get4_codes(t.m, i, have, wide, t.m_scale[block], m);
         get4_codes(t.v, i, have, wide, t.v_scale[block], v);
       } else {
-        get4<float>(t.m, i, have, wide, m);
-        get4<float>(t.v, i, have, wide, v);
+        get4<ONCE, float>(t.m, i, have, wide, m);
+        get4<ONCE, float>(t.v, i, have, wide, v);
       }
     }
 #pragma unroll
@@ -171,12 +188,13 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
       const float gj = g[j] * a.grad_scale;
       m[j] = m[j] * a.beta1 + gj * a.omb1;
       v[j] = v[j] * a.beta2 + (gj * gj) * a.omb2;
-      p[j] = p[j] * a.decay - a.step_size * (m[j] / (sqrtf(v[j]) * a.root + a.eps));
+      // the step may be off by a few units in its last place (the states may not: they are held in codes)
+      p[j] = p[j] * a.decay - a.step_size * m[j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[j]) * a.root + a.eps);
       if (j >= have) m[j] = v[j] = 0.f;   // a value past the end has no part in the scale
     }
     if (have > 0) {
-      if (t.master) put4<float>(t.master, i, have, wide, p);
-      put4(t.param_dtype, t.param, i, have, wide, p);
+      if (t.master) put4<ONCE, float>(t.master, i, have, wide, p);
+      put4<ONCE>(t.param_dtype, t.param, i, have, wide, p);
     }
     if constexpr (BITS8) {
       uint32_t rm[4], rv[4];
@@ -190,8 +208,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
       put4_codes<false>(t.m, t.m_scale + block, i, have, wide, m, rm);
       put4_codes<true>(t.v, t.v_scale + block, i, have, wide, v, rv);
     } else if (have > 0) {
-      put4<float>(t.m, i, have, wide, m);
-      put4<float>(t.v, i, have, wide, v);
+      put4<ONCE, float>(t.m, i, have, wide, m);
+      put4<ONCE, float>(t.v, i, have, wide, v);
     }
   }
 }
@@ -200,10 +218,17 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
 
 hipError_t launch_adamw(const AdamArgs& a, int64_t chunks, hipStream_t s) {
   if (chunks <= 0) return hipSuccess;
-  if (a.bits8)
-    adamw_kernel<true><<<dim3((unsigned)chunks), kThreads, 0, s>>>(a);
+  // 16 M elements and their states pass the 256 MB that the caches hold
+  const bool once = chunks * a.chunk >= (int64_t(1) << 24);
+  const dim3 grid((unsigned)chunks);
+  if (a.bits8 && once)
+    adamw_kernel<true, true><<<grid, kThreads, 0, s>>>(a);
+  else if (a.bits8)
+    adamw_kernel<true, false><<<grid, kThreads, 0, s>>>(a);
+  else if (once)
+    adamw_kernel<false, true><<<grid, kThreads, 0, s>>>(a);
   else
-    adamw_kernel<false><<<dim3((unsigned)chunks), kThreads, 0, s>>>(a);
+    adamw_kernel<false, false><<<grid, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

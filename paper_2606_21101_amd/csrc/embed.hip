@@ -716,6 +716,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs& args, hipStream_t s) {
   // a workgroup that zeroes has some 16 KB of it
   const auto zero_blocks = [&](int shares) { return std::min<int64_t>((bytes / shares + 16383) / 16384, 4096); };
   hipError_t e = hipSuccess;
+  if (a.tokens == 0 && bytes == 0) return e;
   if (a.tiles == 1 || a.tokens == 0) {
     a.zero_shares = 1;
     sort_one_kernel<<<dim3((unsigned)(1 + zero_blocks(1))), kSortOneThreads, 0, s>>>(a);

@@ -11,6 +11,8 @@
 
 using namespace dpi;
 
+static_assert(DPI_ADAMW_BLOCK == kAdamBlock, "the scale blocks of the interface");
+
 __attribute__((visibility("hidden"))) dpi_status dpi_fail_status(dpi_status s, const char* fmt, ...);   // api.cpp
 __attribute__((visibility("hidden"))) dpi_status dpi_hip_status(hipError_t e, const char* what);        // api.cpp
 
@@ -121,18 +123,20 @@ GlrArgs glr_args(const dpi_glr_desc* d, void* workspace, int32_t* status) {
 struct dpi_adamw_s {
   std::vector<AdamTensor> tensors;
   std::vector<int64_t> first_chunk;   // [tensors + 1]
-  int32_t bits = 32;
+  int32_t bits = 32, chunk = kAdamChunk;
   const AdamTensor* dev_tensors = nullptr;
   const AdamChunk* dev_chunks = nullptr;
 };
 
 namespace {
 
-// Tensors checked, and their chunks counted.
-dpi_status check_adamw(const dpi_adamw_tensor* tensors, int32_t n, int32_t bits, int64_t& chunks) {
+// Tensors checked, the chunks' size chosen and their number counted.
+dpi_status check_adamw(const dpi_adamw_tensor* tensors, int32_t n, int32_t bits, int32_t& chunk, int64_t& chunks) {
   chunks = 0;
+  chunk = kAdamChunk;
   if (n < 1 || !tensors) return dpi_fail_status(DPI_ERR_INVALID_ARG, "no tensors");
   if (bits != 32 && bits != 8) return dpi_fail_status(DPI_ERR_INVALID_ARG, "state_bits must be 32 or 8");
+  int64_t total = 0;
   for (int32_t i = 0; i < n; ++i) {
     const dpi_adamw_tensor& t = tensors[i];
     if (t.count < 0) return dpi_fail_status(DPI_ERR_INVALID_ARG, "tensor %d: negative count", i);
@@ -145,9 +149,12 @@ dpi_status check_adamw(const dpi_adamw_tensor* tensors, int32_t n, int32_t bits,
         (bits == 32 && (off_by(t.m, 4) || off_by(t.v, 4))))
       return dpi_fail_status(DPI_ERR_MISALIGNED, "tensor %d not element-aligned", i);
     if (t.count > (int64_t(1) << 42)) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "tensor %d too large", i);
-    chunks += (t.count + kAdamChunk - 1) / kAdamChunk;
-    if (chunks > INT32_MAX) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "tensors too large");
+    total += t.count;
+    if (total > (int64_t(1) << 42)) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "tensors too large");
   }
+  if (total <= kAdamFew) chunk = kAdamFewChunk;
+  for (int32_t i = 0; i < n; ++i) chunks += (tensors[i].count + chunk - 1) / chunk;
+  if (chunks > INT32_MAX) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "too many tensors");
   return DPI_OK;
 }
 
@@ -343,7 +350,8 @@ dpi_status dpi_glr_step(const void* x, int64_t x_stride, const void* gate, int64
 
 size_t dpi_adamw_workspace_bytes(const dpi_adamw_tensor* tensors, int32_t num_tensors, int32_t state_bits) {
   int64_t chunks = 0;
-  if (check_adamw(tensors, num_tensors, state_bits, chunks) != DPI_OK) return 0;
+  int32_t chunk = 0;
+  if (check_adamw(tensors, num_tensors, state_bits, chunk, chunks) != DPI_OK) return 0;
   return adamw_table_bytes(num_tensors) + std::max<size_t>(16, (size_t)chunks * sizeof(AdamChunk));
 }
 
@@ -352,7 +360,8 @@ dpi_status dpi_adamw_create(const dpi_adamw_tensor* tensors, int32_t num_tensors
   if (!out) return dpi_fail_status(DPI_ERR_INVALID_ARG, "out is NULL");
   *out = nullptr;
   int64_t chunks = 0;
-  DPI_TRY(check_adamw(tensors, num_tensors, state_bits, chunks));
+  int32_t chunk = 0;
+  DPI_TRY(check_adamw(tensors, num_tensors, state_bits, chunk, chunks));
   DPI_TRY(check_workspace(workspace, workspace_bytes, dpi_adamw_workspace_bytes(tensors, num_tensors, state_bits)));
   dpi_adamw_s* h = nullptr;
   try {
@@ -365,10 +374,11 @@ dpi_status dpi_adamw_create(const dpi_adamw_tensor* tensors, int32_t num_tensors
       const dpi_adamw_tensor& t = tensors[i];
       h->tensors.push_back(AdamTensor{t.param, t.master, t.m, t.v, t.m_scale, t.v_scale, t.count, t.param_dtype, t.grad_dtype});
       h->first_chunk.push_back((int64_t)map.size());
-      for (int64_t c = 0; c * kAdamChunk < t.count; ++c) map.push_back(AdamChunk{i, (int32_t)c});
+      for (int64_t c = 0; c * chunk < t.count; ++c) map.push_back(AdamChunk{i, (int32_t)c});
     }
     h->first_chunk.push_back((int64_t)map.size());
     h->bits = state_bits;
+    h->chunk = chunk;
     char* ws = static_cast<char*>(workspace);
     h->dev_tensors = reinterpret_cast<const AdamTensor*>(ws);
     h->dev_chunks = reinterpret_cast<const AdamChunk*>(ws + adamw_table_bytes(num_tensors));
@@ -405,6 +415,7 @@ dpi_status dpi_adamw_step(dpi_adamw_t adamw, const void* const* grads, const dpi
   a.tensors = adamw->dev_tensors;
   a.chunks = adamw->dev_chunks;
   a.bits8 = adamw->bits == 8;
+  a.chunk = adamw->chunk;
   a.beta1 = (float)y.beta1;
   a.beta2 = (float)y.beta2;
   a.omb1 = (float)(1.0 - y.beta1);

@@ -12,7 +12,13 @@ from typing import Optional, Sequence
 import torch
 
 from . import dpi
-from .sequence import _DT, _dtype, _here, _on, _refuse
+from .sequence import _DT, _here, _on, _refuse
+
+
+def _code(dtype: torch.dtype) -> int:
+    if dtype not in _DT:
+        _refuse(f"gradients of {dtype}")
+    return _DT[dtype]
 
 
 class AdamW:
@@ -20,7 +26,8 @@ class AdamW:
     all of them, a list of such copies, or None.  state_bits 8: m and v are e4m3
     values with a float32 scale for every 256 elements (m_scale, v_scale), rounded
     at random from `seed`, the step and the element.  m, v, m_scale, v_scale: the
-    states to go on from (lists of tensors, updated in place), zeros without."""
+    states to go on from (lists of tensors, updated in place), zeros without.
+    The tensors' memory must stay where it is while the object is used."""
 
     def __init__(self, params: Sequence[torch.Tensor], masters=None, state_bits: int = 32, m=None, v=None,
                  m_scale=None, v_scale=None, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -47,7 +54,9 @@ class AdamW:
             self.m_scale = list(m_scale) if m_scale is not None else scales()
             self.v_scale = list(v_scale) if v_scale is not None else scales()
         self._check(held, blocks)
-        self._grad_dtypes = None
+        self._counts = [p.numel() for p in self.params]
+        self._pointers = ctypes.c_void_p * len(self.params)
+        self._grad_dtypes = [p.dtype for p in self.params]   # until gradients of others come
         self._handle = None
 
     def _check(self, held, blocks) -> None:
@@ -85,7 +94,7 @@ class AdamW:
             arr[i] = dpi.dpi_adamw_tensor(
                 p.data_ptr(), self.masters[i].data_ptr() if self.masters else None, self.m[i].data_ptr(),
                 self.v[i].data_ptr(), self.m_scale[i].data_ptr() if self.m_scale else None,
-                self.v_scale[i].data_ptr() if self.v_scale else None, p.numel(), _DT[p.dtype], _DT[grad_dtypes[i]])
+                self.v_scale[i].data_ptr() if self.v_scale else None, p.numel(), _DT[p.dtype], _code(grad_dtypes[i]))
         need = dpi.dpi_adamw_workspace_bytes(arr, self.state_bits)
         if need == 0:
             raise dpi.DpiError(dpi.DPI_ERR_INVALID_ARG, dpi.dpi_last_error())
@@ -93,8 +102,6 @@ class AdamW:
         torch.cuda.synchronize(self.device)   # ... and its memory may have been another tensor's until now
         self._handle = dpi.dpi_adamw_create(arr, self.state_bits, self._ws)
         self._grad_dtypes = grad_dtypes
-        self._counts = [p.numel() for p in self.params]
-        self._grads = (ctypes.c_void_p * n)()
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, step: Optional[int] = None,
              lr: Optional[float] = None, grad_scale: float = 1.0, stream=None) -> None:
@@ -104,28 +111,23 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if len(grads) != len(self.params):
             _refuse("one gradient a parameter")
-        _here(self.device)
-        held = self._grad_dtypes or [p.dtype for p in self.params]
-        dtypes = [g.dtype if g is not None else d for g, d in zip(grads, held)]
-        if dtypes != self._grad_dtypes:
-            for g in grads:
-                if g is not None:
-                    _dtype(g, "gradient")
+        _here(self.params[0])
+        held = self._grad_dtypes
+        dtypes = [d if g is None else g.dtype for g, d in zip(grads, held)]
+        if self._handle is None or dtypes != held:
             self._create(dtypes)
+        index = torch.cuda.current_device()
         for i, (g, n) in enumerate(zip(grads, self._counts)):
-            if g is None:
-                self._grads[i] = None
-                continue
-            if g.numel() != n or g.device != self.device or not g.is_contiguous():
+            if g is not None and (g.numel() != n or g.get_device() != index or not g.is_contiguous()):
                 _refuse(f"gradient {i} must be contiguous, of the parameter's size, on {self.device}")
-            self._grads[i] = g.data_ptr()
+        array = self._pointers(*[None if g is None else g.data_ptr() for g in grads])
         t = self.step_count + 1 if step is None else int(step)
         hyper = dpi.dpi_adamw_hyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps,
                                     self.weight_decay, grad_scale, t, self.seed & 0xFFFFFFFF)
         handle, _ = _on(stream)
         if stream is not None:
             self._ws.record_stream(torch.cuda.ExternalStream(handle))
-        dpi.dpi_adamw_step(self._handle, self._grads, hyper, handle)
+        dpi.dpi_adamw_step(self._handle, array, hyper, handle)
         self.step_count = t
 
     def _destroy(self) -> None:

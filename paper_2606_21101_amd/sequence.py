@@ -31,13 +31,12 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return code
 
 
-def _here(device: torch.device, *tensors) -> None:
-    """All of them on `device`, which has to be the current one."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        _refuse(f"{device} is not the current GPU")
+def _here(*tensors) -> None:
+    """All of them on the current GPU."""
+    index = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.device != device:
-            _refuse(f"a tensor is on {t.device}, not {device}")
+        if t is not None and t.get_device() != index:
+            _refuse(f"a tensor is on {t.device}, not on the current GPU ({index})")
 
 
 def _rows(t: torch.Tensor, n: int, dim: int, what: str) -> int:
@@ -62,10 +61,13 @@ def _states(t: Optional[torch.Tensor], n: int, dim: int, what: str) -> Optional[
     return t
 
 
+_NO_CONTEXT = contextlib.nullcontext()
+
+
 def _on(stream):
     """The stream to use, and the context in which its memory is allocated."""
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream, contextlib.nullcontext()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()), _NO_CONTEXT
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream)
     return stream.cuda_stream, torch.cuda.stream(stream)
@@ -111,7 +113,7 @@ class SequenceEmbedding:
         if out is None:
             with context:
                 out = torch.empty((n, self.dim), dtype=self.out_dtype, device=self.table.device)
-        _here(self.table.device, ids, out, self.status)
+        _here(self.table, ids, out, self.status)
         if out.dtype != self.out_dtype:
             _refuse(f"out: dtype {out.dtype}, not {self.out_dtype}")
         dpi.dpi_embed_forward(self.table, self._code, self.num_rows, self.dim, ids, n, self.scale, self.padding_id,
@@ -128,7 +130,7 @@ class SequenceEmbedding:
             if grad is None:
                 grad = torch.empty_like(self.table)
             ws = self._ws.get(handle, dpi.dpi_embed_workspace_bytes(self.num_rows, self.dim, n), self.table.device)
-        _here(self.table.device, ids, dout, grad, self.status)
+        _here(self.table, ids, dout, grad, self.status)
         if tuple(grad.shape) != (self.num_rows, self.dim) or not grad.is_contiguous():
             _refuse(f"grad must be a contiguous {(self.num_rows, self.dim)} tensor")
         dpi.dpi_embed_backward(dout, _dtype(dout, "dout"), _rows(dout, n, self.dim, "dout"), ids, n, self.scale,
@@ -201,7 +203,7 @@ class GatedRecurrence:
             h_last = torch.empty((desc.num_seqs, self.dim), dtype=torch.float32, device=x.device)
             entry = torch.empty(dpi.dpi_glr_entry_bytes(desc) // 4, dtype=torch.float32, device=x.device) if save else None
             ws = self._ws.get(handle, dpi.dpi_glr_workspace_bytes(desc), x.device)
-        _here(x.device, gate, offsets, h0, out, self.status)
+        _here(x, gate, offsets, h0, out, self.status)
         if out.dtype != x.dtype:
             _refuse("out must have x's dtype")
         dpi.dpi_glr_forward(desc, out, _rows(out, desc.num_tokens, self.dim, "out"), h_last, entry, ws, None,
@@ -224,7 +226,7 @@ class GatedRecurrence:
                 dgate = torch.empty((n, self.dim), dtype=x.dtype, device=x.device)
             dh0 = torch.empty((seqs, self.dim), dtype=torch.float32, device=x.device)
             ws = self._ws.get(handle, dpi.dpi_glr_workspace_bytes(desc), x.device)
-        _here(x.device, dh, dh_last, dx, dgate, self.status)
+        _here(x, dh, dh_last, dx, dgate, self.status)
         for t, what in ((dh, "dh"), (dx, "dx"), (dgate, "dgate")):
             if t is not None and t.dtype != x.dtype:
                 _refuse(f"{what} must have x's dtype")
@@ -250,7 +252,7 @@ class GatedRecurrence:
         if out is None:
             with context:
                 out = torch.empty((n, self.dim), dtype=x.dtype, device=x.device)
-        _here(x.device, gate, state, slots, out, self.status)
+        _here(x, gate, state, slots, out, self.status)
         if out.dtype != x.dtype:
             _refuse("out must have x's dtype")
         dpi.dpi_glr_step(x, _rows(x, n, self.dim, "x"), gate, _rows(gate, n, self.dim, "gate"), _dtype(x, "x"), n,

@@ -114,7 +114,7 @@ def store8(x, rnd, keep_small):
     top = np.abs(y).max(1)
     held = top > f(2.0 ** -100)
     with np.errstate(divide="ignore"):
-        inv, scale = np.where(held, f(448) / top, f(0)), np.where(held, top / f(448), f(0))
+        inv, scale = np.where(held, (f(1) / top) * f(448), f(0)), np.where(held, top * (f(1) / f(448)), f(0))
     z = np.minimum(np.abs(y) * inv[:, None], f(448))
     normal = ((z.view(np.int32).astype(np.int64) + r) >> 20) - (120 << 3)
     small = np.floor(z * f(512) + r.astype(f) * f(2.0 ** -20)).astype(np.int64)

@@ -53,7 +53,7 @@ EMBED = [   # tokens, rows, dim, table, out, law, wide
     (64, 100, 10, "f16", "f32", "zipf", 0), (65, 100, 50, "f16", "f16", "zipf", 2), (1000, 300, 64, "f32", "bf16", "zipf", 0),
     (4097, 1000, 60, "f32", "f32", "zipf", 4), (5000, 257, 128, "bf16", "bf16", "one", 0), (3000, 70000, 33, "f16", "f32", "uniform", 1),
     (2000, 50, 200, "bf16", "f32", "zipf", 8), (700, 20, 1000, "f16", "f16", "uniform", 0), (129, 20, 513, "f32", "f32", "zipf", 0),
-    (20000, 3, 8, "f16", "f32", "uniform", 0), (9000, 2_000_000, 4, "f32", "f32", "uniform", 0),
+    (20000, 3, 8, "f16", "f32", "uniform", 0), (20000, 9, 256, "f32", "f32", "one", 0), (9000, 2_000_000, 4, "f32", "f32", "uniform", 0),
 ]
 
 
