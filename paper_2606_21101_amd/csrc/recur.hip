@@ -399,24 +399,24 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
     }
   }
   const bool last = UP ? p.lane >= 64 - p.lc : p.lane < p.lc;
-  float* const all_a = maps + p.c * V;
-  float* const all_s = all_a + kWaves * V * p.lc;
+  typedef float quad __attribute__((ext_vector_type(4)));
+  static_assert(V == 4, "a thread's channels are one 16-byte access");
+  quad* const all_a = reinterpret_cast<quad*>(maps) + p.c;   // [waves][LC]
+  quad* const all_s = all_a + kWaves * p.lc;
   if (last) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      all_a[p.wave * V * p.lc + v] = A[v];
-      all_s[p.wave * V * p.lc + v] = S[v];
-    }
+    all_a[p.wave * p.lc] = quad{A[0], A[1], A[2], A[3]};
+    all_s[p.wave * p.lc] = quad{S[0], S[1], S[2], S[3]};
   }
   __syncthreads();
   float mine[V];
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
     const int w = UP ? i : kWaves - 1 - i;
+    const quad wa = all_a[w * p.lc], ws = all_s[w * p.lc];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (w == p.wave) mine[v] = state[v];
-      state[v] = mul0(all_a[w * V * p.lc + v], state[v]) + all_s[w * V * p.lc + v];
+      state[v] = mul0(wa[v], state[v]) + ws[v];
     }
   }
   const bool first = UP ? p.lane < p.lc : p.lane >= 64 - p.lc;
@@ -865,12 +865,12 @@ GlrShape glr_shape(int64_t tokens, int32_t dim) {
   return sh;
 }
 
-GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len) {
+GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len, bool backward) {
   const GlrShape sh = glr_shape(tokens, dim);
   GlrSplit sp{};
   const int64_t longest = max_len > 0 ? std::min(max_len, tokens) : tokens;
   sp.cut = longest > kGlrWholeBlocks * sh.block_tokens;
-  const int64_t groups = kGlrGroups / sh.channel_blocks + 1;
+  const int64_t groups = std::max<int64_t>(1, (backward ? kGlrBackwardGroups : kGlrGroups) / sh.channel_blocks);
   const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (sh.blocks + groups - 1) / groups), kGlrRangeBlocks);
   sp.range = blocks * sh.block_tokens;
   sp.units = (tokens + sp.range - 1) / sp.range;

@@ -95,7 +95,7 @@ struct Wide {
   void add(const void* p, int64_t stride) { ok = ok && !off_by(p, access) && ((size_t)stride * elem) % access == 0; }
 };
 
-GlrArgs glr_args(const dpi_glr_desc* d, void* workspace, int32_t* status) {
+GlrArgs glr_args(const dpi_glr_desc* d, bool backward, void* workspace, int32_t* status) {
   GlrArgs a{};
   a.offsets = d->offsets;
   a.x = d->x;
@@ -109,7 +109,7 @@ GlrArgs glr_args(const dpi_glr_desc* d, void* workspace, int32_t* status) {
   a.dim = d->dim;
   a.dtype = d->dtype;
   a.lc_log = glr_shape(d->num_tokens, d->dim).lc_log;
-  const GlrSplit sp = glr_split(d->num_tokens, d->dim, d->max_len);
+  const GlrSplit sp = glr_split(d->num_tokens, d->dim, d->max_len, backward);
   a.cut = sp.cut;
   a.range = sp.range;
   a.units = sp.units;
@@ -243,8 +243,12 @@ size_t dpi_glr_entry_bytes(const dpi_glr_desc* desc) {
 
 size_t dpi_glr_workspace_bytes(const dpi_glr_desc* desc) {
   if (check_glr(desc) != DPI_OK) return 0;
-  const GlrSplit sp = glr_split(desc->num_tokens, desc->dim, desc->max_len);
-  return sp.cut ? std::max<size_t>(16, (size_t)sp.units * (size_t)desc->dim * 2 * sizeof(float)) : 16;
+  size_t most = 16;
+  for (const bool backward : {false, true}) {
+    const GlrSplit sp = glr_split(desc->num_tokens, desc->dim, desc->max_len, backward);
+    if (sp.cut) most = std::max(most, (size_t)sp.units * (size_t)desc->dim * 2 * sizeof(float));
+  }
+  return most;
 }
 
 dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, float* h_last, void* entry,
@@ -256,7 +260,7 @@ dpi_status dpi_glr_forward(const dpi_glr_desc* desc, void* h, int64_t h_stride, 
   DPI_TRY(check_words(entry, false, "entry"));
   DPI_TRY(check_words(device_status, false, "device_status"));
   DPI_TRY(check_workspace(workspace, workspace_bytes, dpi_glr_workspace_bytes(desc)));
-  GlrArgs a = glr_args(desc, workspace, device_status);
+  GlrArgs a = glr_args(desc, false, workspace, device_status);
   a.h = h;
   a.h_stride = h_stride;
   a.h_last = h_last;
@@ -287,7 +291,7 @@ dpi_status dpi_glr_backward(const dpi_glr_desc* desc, const void* entry, const v
   DPI_TRY(check_words(dh0, false, "dh0"));
   DPI_TRY(check_words(device_status, false, "device_status"));
   DPI_TRY(check_workspace(workspace, workspace_bytes, dpi_glr_workspace_bytes(desc)));
-  GlrArgs a = glr_args(desc, workspace, device_status);
+  GlrArgs a = glr_args(desc, true, workspace, device_status);
   a.entry = static_cast<float*>(const_cast<void*>(entry));
   a.dh = dh;
   a.dh_stride = dh_stride;

@@ -90,8 +90,9 @@ constexpr int kGlrThreads = 256;
 constexpr int kGlrV = 4;              // channels per thread
 constexpr int kGlrK = 4;              // tokens per thread
 constexpr int64_t kGlrMaxStride = 1 << 18;   // row strides are smaller: kGlrThreads * kGlrK rows span less than 2^31 bytes
-constexpr int kGlrGroups = 1024;      // workgroups a pass is split into, while ...
-constexpr int kGlrRangeBlocks = 16;   // ... a range has at most so many blocks
+constexpr int kGlrGroups = 1024;      // workgroups a pass is split into, what 256 CUs hold at once, ...
+constexpr int kGlrBackwardGroups = 768;
+constexpr int kGlrRangeBlocks = 64;   // ... while a range has at most so many blocks
 constexpr int kGlrWholeBlocks = 16;   // the longest sequence that one workgroup walks, in blocks
 
 struct GlrShape {
@@ -104,7 +105,7 @@ struct GlrSplit {
   int32_t cut;
   int64_t range, units;
 };
-GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len);
+GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len, bool backward);
 
 hipError_t launch_glr_forward(const GlrArgs& a, hipStream_t s);
 hipError_t launch_glr_backward(const GlrArgs& a, hipStream_t s);
