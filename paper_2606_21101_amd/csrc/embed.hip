@@ -464,13 +464,31 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradA
   if (!mine) return;
   // a row that begins in this chunk and goes on: the chunks after it, while it goes through them
   const bool first = g == 0 && (how & kRowCut);   // ... and one that began before the span
+  // acc and the heads of the chunks from k on, eight in flight; whether the row is still open after the last
+  const auto add_heads = [&](int k) {
+    for (;; k += 8) {
+      uint32_t how_k[8];
+      float h[8][V];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int ku = min(k + u, groups - 1);
+        how_k[u] = state[ku];
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[u][j] = head[((int)(threadIdx.x & (lpr - 1)) + (ku << sh.lpr_log)) * V + j];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (k + u >= groups) return true;
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += h[u][j];
+        if (!(how_k[u] & kRowThrough)) return false;
+      }
+    }
+  };
   if (first) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] = head[threadIdx.x * V + j];
-    for (int k = 0; k + 1 < groups && (state[k] & kRowThrough); ++k) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] += head[(threadIdx.x + ((k + 1) << sh.lpr_log)) * V + j];
-    }
+    for (int j = 0; j < V; ++j) acc[j] = 0.f;
+    add_heads(0);
     float* part = a.part + (int64_t)blockIdx.x * 2 * a.dim + col;
 #pragma unroll
     for (int j = 0; j < V; ++j) part[j] = acc[j];
@@ -478,13 +496,7 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradA
   if (how & kRowGoesOn) {
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = tail[threadIdx.x * V + j];
-    bool open = true;
-    for (int k = g + 1; k < groups && open; ++k) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] += head[(threadIdx.x + ((k - g) << sh.lpr_log)) * V + j];
-      open = (state[k] & kRowThrough) != 0;
-    }
-    if (open) {   // on into the next span
+    if (add_heads(g + 1)) {   // on into the next span
       float* part = a.part + ((int64_t)blockIdx.x * 2 + 1) * a.dim + col;
 #pragma unroll
       for (int j = 0; j < V; ++j) part[j] = acc[j];

@@ -386,18 +386,31 @@ __device__ __forceinline__ void load_dh(const GlrArgs& a, const Place& p, const 
 // read any more when another comes here.
 template <bool UP>
 __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, float* maps, float* state, float* enter) {
-  for (int d = p.lc; d < 64; d <<= 1) {
+  // a map of the lanes d before (after), all its values on their way at once; the identity where there are none
+  float a0[V], s0[V];
+  const auto neighbour = [&](int d) {
     const bool has = UP ? p.lane >= d : p.lane + d < 64;
+    const int from = (UP ? p.lane - d : p.lane + d) * 4;   // bytes, as the permute takes lanes, modulo the wave
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float s0 = UP ? __shfl_up(S[v], d, 64) : __shfl_down(S[v], d, 64);
-      const float a0 = UP ? __shfl_up(A[v], d, 64) : __shfl_down(A[v], d, 64);
-      if (has) {
-        S[v] = mul0(A[v], s0) + S[v];
-        A[v] *= a0;
-      }
+      s0[v] = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(S[v])));
+      a0[v] = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(A[v])));
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      s0[v] = has ? s0[v] : 0.f;
+      a0[v] = has ? a0[v] : 1.f;
+    }
+  };
+  for (int d = p.lc; d < 64; d <<= 1) {
+    neighbour(d);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      S[v] = mul0(A[v], s0[v]) + S[v];
+      A[v] *= a0[v];
     }
   }
+  neighbour(p.lc);   // what the groups before it make of the state that enters the wave
   const bool last = UP ? p.lane >= 64 - p.lc : p.lane < p.lc;
   typedef float quad __attribute__((ext_vector_type(4)));
   static_assert(V == 4, "a thread's channels are one 16-byte access");
@@ -419,13 +432,8 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
       state[v] = mul0(wa[v], state[v]) + ws[v];
     }
   }
-  const bool first = UP ? p.lane < p.lc : p.lane >= 64 - p.lc;
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const float s0 = UP ? __shfl_up(S[v], p.lc & 63, 64) : __shfl_down(S[v], p.lc & 63, 64);
-    const float a0 = UP ? __shfl_up(A[v], p.lc & 63, 64) : __shfl_down(A[v], p.lc & 63, 64);
-    enter[v] = first ? mine[v] : mul0(a0, mine[v]) + s0;
-  }
+  for (int v = 0; v < V; ++v) enter[v] = mul0(a0[v], mine[v]) + s0[v];
 }
 
 // The edges among a thread's tokens.  The first one's state is in registers, read as soon as the marks are known with the
