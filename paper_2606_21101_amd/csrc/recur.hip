@@ -168,16 +168,17 @@ struct Window {
 // starts / ends: the lane's K tokens of the block at `t0` that are a sequence's first / last; seq_of[i], end_of[i]: that
 // sequence, where it is.  Only tokens of [lo, hi) are marked.
 template <bool FORWARD>
-__device__ __forceinline__ void marks_of(const GlrArgs& a, Window& w, int64_t t0, int tokens, int64_t lo, int64_t hi,
+__device__ __forceinline__ void marks_of(const GlrArgs& a, Window& w, int64_t at, int tokens, int64_t lo, int64_t hi,
                                          int lane, int mine, int32_t* starts_at, int32_t* ends_at, uint32_t& starts,
                                          uint32_t& ends) {
-  const int64_t t1 = t0 + tokens;
+  const int32_t t0 = (int32_t)min(at, (int64_t)INT32_MAX), t1 = (int32_t)min(at + tokens, (int64_t)INT32_MAX);
+  const int32_t first = max(t0, (int32_t)lo), past = min(t1, (int32_t)hi);   // the tokens that may be marked
   starts = ends = 0;
   bool any = false;
   for (;;) {
     const bool full = w.end > w.begin;
-    const bool b = full && w.begin >= max(t0, lo) && w.begin < min(t1, hi);
-    const bool e = full && w.end > max(t0, lo) && w.end <= min(t1, hi);
+    const bool b = full && w.begin >= first && w.begin < past;
+    const bool e = full && w.end > first && w.end <= past;
     if (__ballot(b || e)) {
       if (!any) {
         any = true;
@@ -187,12 +188,10 @@ __device__ __forceinline__ void marks_of(const GlrArgs& a, Window& w, int64_t t0
       if (e) ends_at[w.end - 1 - t0] = (int32_t)(w.base + lane);
     }
     if (FORWARD) {
-      const int32_t far = __builtin_amdgcn_readlane(w.end, 63);
-      if ((int64_t)far > t1 || w.base + 64 >= a.seqs) break;
+      if (__builtin_amdgcn_readlane(w.end, 63) > t1 || w.base + 64 >= a.seqs) break;
       w.load(a, w.base + 64, lane);
     } else {
-      const int32_t far = __builtin_amdgcn_readfirstlane(w.begin);
-      if ((int64_t)far <= t0 || w.base == 0) break;
+      if (__builtin_amdgcn_readfirstlane(w.begin) <= t0 || w.base == 0) break;
       w.load(a, w.base - 63, lane);   // one again: its begin says whether to go on
     }
   }
@@ -381,14 +380,22 @@ __device__ __forceinline__ void load_dh(const GlrArgs& a, const Place& p, const 
   }
 }
 
+// A barrier for what waves exchange in LDS.  __syncthreads() would also wait for the block's stores and the next one's
+// loads, which no other wave looks at.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Threads' maps (A, S) to the state that enters each one's tokens, `enter`; `state`, the one that enters the block, becomes
 // the one that leaves it.  UP: groups and waves in order of time, else against it.  maps: a buffer that no thread has to
 // read any more when another comes here.
 template <bool UP>
 __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, float* maps, float* state, float* enter) {
   // a map of the lanes d before (after), all its values on their way at once; the identity where there are none
-  float a0[V], s0[V];
-  const auto neighbour = [&](int d) {
+  float a0[V], s0[V], pa[V], ps[V];
+  const auto neighbour = [&](int d, const float* A, const float* S) {
     const bool has = UP ? p.lane >= d : p.lane + d < 64;
     const int from = (UP ? p.lane - d : p.lane + d) * 4;   // bytes, as the permute takes lanes, modulo the wave
 #pragma unroll
@@ -402,15 +409,26 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
       a0[v] = has ? a0[v] : 1.f;
     }
   };
-  for (int d = p.lc; d < 64; d <<= 1) {
-    neighbour(d);
+  // pa, ps: the map of the groups before the thread's, the nearest one, then of 2, 4, ... more
+  neighbour(p.lc, A, S);
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    pa[v] = a0[v];
+    ps[v] = s0[v];
+  }
+  for (int d = p.lc; d < 64 - p.lc; d <<= 1) {
+    neighbour(d, pa, ps);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      S[v] = mul0(A[v], s0[v]) + S[v];
-      A[v] *= a0[v];
+      ps[v] = mul0(pa[v], s0[v]) + ps[v];
+      pa[v] *= a0[v];
     }
   }
-  neighbour(p.lc);   // what the groups before it make of the state that enters the wave
+#pragma unroll
+  for (int v = 0; v < V; ++v) {   // with the thread's own, for the wave's last group: the wave's map
+    S[v] = mul0(A[v], ps[v]) + S[v];
+    A[v] *= pa[v];
+  }
   const bool last = UP ? p.lane >= 64 - p.lc : p.lane < p.lc;
   typedef float quad __attribute__((ext_vector_type(4)));
   static_assert(V == 4, "a thread's channels are one 16-byte access");
@@ -420,7 +438,7 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
     all_a[p.wave * p.lc] = quad{A[0], A[1], A[2], A[3]};
     all_s[p.wave * p.lc] = quad{S[0], S[1], S[2], S[3]};
   }
-  __syncthreads();
+  lds_barrier();
   float mine[V];
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
@@ -433,7 +451,7 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
     }
   }
 #pragma unroll
-  for (int v = 0; v < V; ++v) enter[v] = mul0(a0[v], mine[v]) + s0[v];
+  for (int v = 0; v < V; ++v) enter[v] = mul0(pa[v], mine[v]) + ps[v];
 }
 
 // The edges among a thread's tokens.  The first one's state is in registers, read as soon as the marks are known with the
