@@ -681,7 +681,10 @@ hipError_t sums_by_piece(const EmbedGradArgs& a, hipStream_t s) {
     return a.dim % w == 0 && (reinterpret_cast<uintptr_t>(a.dout) & in) == 0 && (a.dout_stride * sizeof(TIN) & in) == 0 &&
            (reinterpret_cast<uintptr_t>(a.grad) & out) == 0 && (a.dim * eg & out) == 0;
   };
-  while (v > 1 && !fits(v)) v >>= 1;
+  // Narrow rows still take 4 lanes: with one lane a row, a workgroup's 256 chunks are a long span, of which few lists have
+  // many, and the rows that go through all of them a long way to join (105,209 tokens of 8 fp16 over 513 rows:
+  // the sums take 27 us with a lane a row, 11.4 with four).
+  while (v > 1 && (!fits(v) || a.dim < 4 * v)) v >>= 1;
   switch (v) {
     case 8: if constexpr (sizeof(TIN) == 2) return run_sums<TIN, 8>(a, s);
     case 4: return run_sums<TIN, 4>(a, s);
