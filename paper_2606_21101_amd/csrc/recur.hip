@@ -351,14 +351,22 @@ struct Rows {
   }
 };
 
-// The thread's rows of one operand; those outside the span are `other`.
+// The thread's rows of one operand; those outside the span are `other`, and not read.
 template <bool WIDE, typename T>
 __device__ __forceinline__ void load_block(const void* from, int64_t stride, const Place& p, const Block& b, float other,
                                            Elems<T, V>* e) {
-  const Rows<WIDE, T> rows(from, stride, p, b);
+  Rows<WIDE, T> rows(from, stride, p, b);
+  if (b.whole) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) e[k] = rows.get(k);
-  if (b.whole) return;
+    for (int k = 0; k < K; ++k) e[k] = rows.get(k);
+    return;
+  }
+  const int32_t lane = rows.lane;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    rows.lane = b.has(p.row + k) ? lane : 0x7fff0000;   // past any end: no access
+    e[k] = rows.get(k);
+  }
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     if (b.has(p.row + k)) continue;
