@@ -10,9 +10,9 @@
 // registers, groups join their maps by shuffles, waves by LDS, and each thread
 // walks its tokens again from the state that enters them.
 //
-// A sequence's first token is the map with A = 0.  Products with such an A are
-// legacy ones, where 0 times anything is 0: no infinity and no NaN of one
-// sequence gets into the next.  So is (1 - a) x, where a token of gate +inf
+// A sequence's first token is the map with A = 0.  Products with such an A, of
+// two of them too, are legacy ones, where 0 times anything is 0: no infinity and
+// no NaN of one sequence, its gates' among them, gets into the next.  So is (1 - a) x, where a token of gate +inf
 // keeps the state whatever x it has.
 //
 // Work is split in one of two ways.  Whole: a workgroup takes the sequences that
@@ -288,8 +288,8 @@ struct Block {
 };
 
 // The block's rows of a [tokens, dim] operand through a buffer descriptor of its rows up to `past`: a thread keeps one
-// 32-bit offset, its k-th row is a scalar one (64-bit addresses of every row took 40 registers more), and rows past the
-// span are not touched.  A block's rows span less than 2^31 bytes (kGlrMaxStride).
+// 32-bit offset, its k-th row is a scalar one (64-bit addresses of every row took 40 registers more), and rows outside
+// the span are not touched.  A block's rows span less than 2^31 bytes (kGlrMaxStride).
 template <bool WIDE, typename T>
 struct Rows {
   __amdgpu_buffer_rsrc_t rsrc;
@@ -303,24 +303,25 @@ struct Rows {
     // a thread without channels reads the row's first ones
     lane = at.row * stride + (at.have > 0 ? at.ch * (int32_t)sizeof(T) : 0);
   }
-  __device__ __forceinline__ Elems<T, V> get(int k) const {
+  // V channels at byte `at` of the row that begins `row` bytes into the operand
+  __device__ __forceinline__ Elems<T, V> get(int32_t at, int32_t row) const {
     Elems<T, V> e;
     if constexpr (WIDE) {
       if constexpr (sizeof(T) * V == 16) {
         typedef int quad __attribute__((ext_vector_type(4)));
-        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (quad)__builtin_amdgcn_raw_buffer_load_b128(rsrc, lane, k * stride, 0));
+        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (quad)__builtin_amdgcn_raw_buffer_load_b128(rsrc, at, row, 0));
       } else {
         typedef int pair __attribute__((ext_vector_type(2)));
-        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (pair)__builtin_amdgcn_raw_buffer_load_b64(rsrc, lane, k * stride, 0));
+        e.raw = __builtin_bit_cast(typename Raw<T, V>::plain, (pair)__builtin_amdgcn_raw_buffer_load_b64(rsrc, at, row, 0));
       }
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int32_t at = lane + min(v, max(have, 1) - 1) * (int32_t)sizeof(T);
+        const int32_t one = at + min(v, max(have, 1) - 1) * (int32_t)sizeof(T);
         if constexpr (sizeof(T) == 4)
-          e.raw[v] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, k * stride, 0));
+          e.raw[v] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rsrc, one, row, 0));
         else
-          e.raw[v] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, k * stride, 0));
+          e.raw[v] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, one, row, 0));
       }
     }
     return e;
@@ -355,18 +356,15 @@ struct Rows {
 template <bool WIDE, typename T>
 __device__ __forceinline__ void load_block(const void* from, int64_t stride, const Place& p, const Block& b, float other,
                                            Elems<T, V>* e) {
-  Rows<WIDE, T> rows(from, stride, p, b);
+  const Rows<WIDE, T> rows(from, stride, p, b);
   if (b.whole) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) e[k] = rows.get(k);
+    for (int k = 0; k < K; ++k) e[k] = rows.get(rows.lane, k * rows.stride);
     return;
   }
-  const int32_t lane = rows.lane;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    rows.lane = b.has(p.row + k) ? lane : 0x7fff0000;   // past any end: no access
-    e[k] = rows.get(k);
-  }
+  for (int k = 0; k < K; ++k)   // past any end: no access
+    e[k] = rows.get(b.has(p.row + k) ? rows.lane + k * rows.stride : 0x7fff0000, 0);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     if (b.has(p.row + k)) continue;
@@ -429,13 +427,13 @@ __device__ __forceinline__ void join_groups(const Place& p, float* A, float* S, 
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       ps[v] = mul0(pa[v], s0[v]) + ps[v];
-      pa[v] *= a0[v];
+      pa[v] = mul0(pa[v], a0[v]);
     }
   }
 #pragma unroll
   for (int v = 0; v < V; ++v) {   // with the thread's own, for the wave's last group: the wave's map
     S[v] = mul0(A[v], ps[v]) + S[v];
-    A[v] *= pa[v];
+    A[v] = mul0(A[v], pa[v]);
   }
   const bool last = UP ? p.lane >= 64 - p.lc : p.lane < p.lc;
   typedef float quad __attribute__((ext_vector_type(4)));
@@ -740,7 +738,7 @@ __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) prod[v] *= maps[(i * p.lc + p.c) * V + v];
+        for (int v = 0; v < V; ++v) prod[v] = mul0(maps[(i * p.lc + p.c) * V + v], prod[v]);
       }
     }
   }
@@ -783,7 +781,7 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
   if (ch < a.dim)
     walk([&](int64_t, float ma, float ms) {
       S = mul0(ma, S) + ms;
-      A *= ma;
+      A = mul0(ma, A);
     });
   // the groups of a wave, then the waves
 #pragma unroll
@@ -791,7 +789,7 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
     const float s0 = __shfl_up(S, d, 64), a0 = __shfl_up(A, d, 64);
     if (lane >= d) {
       S = mul0(A, s0) + S;
-      A *= a0;
+      A = mul0(A, a0);
     }
   }
   if (lane >= 64 - kScanChannels) {

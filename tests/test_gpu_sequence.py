@@ -282,6 +282,42 @@ def test_masked_tokens_keep_the_state_and_values_that_are_not_finite_stay_in_the
     assert torch.isfinite(y[: off[2]]).all() and torch.isfinite(y[off[3]:]).all()
 
 
+@pytest.mark.parametrize("max_len", [0, 16])
+@pytest.mark.parametrize("dim,dt", [(64, "f32"), (300, "f16"), (7, "bf16"), (256, "bf16")])
+def test_nan_gates_and_gradients_stay_in_their_sequence(dim, dt, max_len):
+    """Every second sequence has NaN gates, rows, states or gradients: the others' results are what they are without."""
+    lens = [3, 5, 1, 30, 2, 200, 17, 600, 5, 9, 1, 4, 70, 1500, 40, 0, 33, 3, 3, 3, 64, 64, 900]
+    off, n = offsets_of(lens), sum(lens)
+    rng = np.random.default_rng(dim)
+    x, g, dh = (tensor(rng.standard_normal((n, dim)), dt) for _ in range(3))
+    h0, dl = (tensor(rng.standard_normal((len(lens), dim)), "f32") for _ in range(2))
+    offsets = torch.from_numpy(off).cuda()
+    op = GatedRecurrence(dim, max_len=max_len)
+
+    def run():
+        y, last, saved = op.forward(x, g, offsets, h0, save=True)
+        return [y, last, *op.backward(saved, dh, dl)]
+
+    good = run()
+    nan = float("nan")
+    odd = torch.arange(len(lens), device="cuda") % 2 == 1
+    rows = torch.repeat_interleave(odd, torch.tensor(lens, device="cuda"))
+    for s in range(1, len(lens), 2):
+        if lens[s] == 0:
+            continue
+        first, last = off[s], off[s + 1] - 1
+        for t in (first, last, (first + last) // 2):
+            g[t] = nan
+        if s % 4 == 1:
+            x[last], dh[first], h0[s], dl[s] = nan, nan, nan, nan
+    got = run()
+    for name, a, b in zip(("h", "h_last", "dx", "dgate", "dh0"), got, good):
+        others = ~rows if len(a) == n else ~odd
+        assert torch.equal(a[others], b[others]), name
+        poisoned = off[1:-1:2][np.asarray(lens[1::2]) > 0] if len(a) == n and name != "dx" else []
+        assert torch.isnan(a[torch.as_tensor(poisoned, dtype=torch.long, device="cuda")]).all(), name
+
+
 def test_malformed_offsets_are_reported():
     x = torch.ones((100, 8), device="cuda")
     for off in ([0, 50, 40, 100], [1, 50, 60, 100], [0, 50, 60, 90]):
