@@ -218,7 +218,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamArgs a) {
 
 hipError_t launch_adamw(const AdamArgs& a, int64_t chunks, hipStream_t s) {
   if (chunks <= 0) return hipSuccess;
-  // 16 M elements and their states pass the 256 MB that the caches hold
+  // 16 M elements and their states pass the 256 MB that the caches hold.  Past them / through them, us: 10 M elements 58 / 53
+  // (8-bit states 35 / 34), 33 M 172 / 186 (97 / 110), 665 M 3,479 / 3,586 (1,982 / 2,082).
   const bool once = chunks * a.chunk >= (int64_t(1) << 24);
   const dim3 grid((unsigned)chunks);
   if (a.bits8 && once)

@@ -876,12 +876,25 @@ hipError_t run_by_dtype(const GlrArgs& a, bool backward, hipStream_t s) {
 
 template <typename T>
 hipError_t run_step(const GlrStepArgs& a, hipStream_t s) {
-  const int64_t threads = a.batch * ((a.dim + V - 1) / V);
-  const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
-  if (a.wide)
-    glr_step_kernel<true, T><<<grid, kThreads, 0, s>>>(a);
-  else
-    glr_step_kernel<false, T><<<grid, kThreads, 0, s>>>(a);
+  const int64_t pieces = (a.dim + V - 1) / V, most = kMostGroups * kThreads / pieces;   // rows of a launch
+  for (int64_t b = 0; b < a.batch; b += most) {
+    GlrStepArgs part = a;
+    part.x = static_cast<const T*>(a.x) + b * a.x_stride;
+    part.gate = static_cast<const T*>(a.gate) + b * a.gate_stride;
+    part.h = static_cast<T*>(a.h) + b * a.h_stride;
+    part.batch = std::min(a.batch - b, most);
+    if (a.slots) {
+      part.slots = a.slots + b;
+    } else {   // the rows that have a state, and no more
+      part.state = a.state + std::min(b, a.num_slots) * a.dim;
+      part.num_slots = std::max<int64_t>(a.num_slots - b, 0);
+    }
+    const dim3 grid((unsigned)((part.batch * pieces + kThreads - 1) / kThreads));
+    if (a.wide)
+      glr_step_kernel<true, T><<<grid, kThreads, 0, s>>>(part);
+    else
+      glr_step_kernel<false, T><<<grid, kThreads, 0, s>>>(part);
+  }
   return hipGetLastError();
 }
 
@@ -897,15 +910,22 @@ GlrShape glr_shape(int64_t tokens, int32_t dim) {
   return sh;
 }
 
+// A range is the work split over kGlrGroups (kGlrBackwardGroups) workgroups.  Cut, the longest sequence is walked a range
+// at a time but its map's tokens are read twice, in three launches; whole, one workgroup walks it to its end.  Cut where
+// that takes more than 6 blocks and 1.5 ranges (backward, where a block takes longer: 4 and 0.5).  Measured in bf16 of 64
+// channels, blocks of 64 tokens, us cut / whole:
+//   longest, range in blocks:  6, 1       8, 1       8, 4       12, 4      16, 4
+//   forward                    20 / 19    20 / 23    47 / 37    48 / 47    48 / 54
+//   and backward               41 / 51    42 / 63    114 / 111  113 / 124  112 / 145
 GlrSplit glr_split(int64_t tokens, int32_t dim, int64_t max_len, bool backward) {
   const GlrShape sh = glr_shape(tokens, dim);
   GlrSplit sp{};
-  const int64_t longest = max_len > 0 ? std::min(max_len, tokens) : tokens;
-  sp.cut = longest > kGlrWholeBlocks * sh.block_tokens;
   const int64_t groups = std::max<int64_t>(1, (backward ? kGlrBackwardGroups : kGlrGroups) / sh.channel_blocks);
   const int64_t blocks = std::min<int64_t>(std::max<int64_t>(1, (sh.blocks + groups - 1) / groups), kGlrRangeBlocks);
   sp.range = blocks * sh.block_tokens;
   sp.units = (tokens + sp.range - 1) / sp.range;
+  const int64_t longest = max_len > 0 ? std::min(max_len, tokens) : tokens;
+  sp.cut = 2 * longest > (backward ? 8 + blocks : 12 + 3 * blocks) * sh.block_tokens;
   return sp;
 }
 

@@ -154,7 +154,7 @@ dpi_status check_adamw(const dpi_adamw_tensor* tensors, int32_t n, int32_t bits,
   }
   if (total <= kAdamFew) chunk = kAdamFewChunk;
   for (int32_t i = 0; i < n; ++i) chunks += (tensors[i].count + chunk - 1) / chunk;
-  if (chunks > INT32_MAX) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "too many tensors");
+  if (chunks > kMostGroups) return dpi_fail_status(DPI_ERR_UNSUPPORTED, "too many tensors");
   return DPI_OK;
 }
 

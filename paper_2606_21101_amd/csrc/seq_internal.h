@@ -9,6 +9,8 @@
 
 namespace dpi {
 
+constexpr int64_t kMostGroups = 1 << 23;   // workgroups of 256 threads of a launch: its threads are counted in 32 bits
+
 // ---------------------------------------------------------------- embedding
 struct EmbedArgs {
   const void* table;
@@ -25,10 +27,10 @@ struct EmbedArgs {
 constexpr int kSortThreads = 256;
 constexpr int kSortMaxBits = 10;                            // bits of a digit
 constexpr int kSortFewItems = 4, kSortManyItems = 16;       // items per thread ...
-constexpr int64_t kSortFewTokens = 1 << 19;                 // ... up to this many tokens, beyond
+constexpr int64_t kSortFewTokens = 3 << 18;                 // ... up to this many tokens, beyond
 constexpr int kSortOneThreads = 1024, kSortOneItems = 4;    // the workgroup that sorts a short list alone
 constexpr int kSumThreads = 256;
-constexpr int kSumMaxChunk = 32;                            // most sorted tokens that one group of lanes sums
+constexpr int kSumMaxChunk = 32;                            // sorted tokens that one group of lanes sums
 
 struct EmbedGradArgs {
   const void* dout;
@@ -93,7 +95,6 @@ constexpr int64_t kGlrMaxStride = 1 << 18;   // row strides are smaller: kGlrThr
 constexpr int kGlrGroups = 1024;      // workgroups a pass is split into, what 256 CUs hold at once, ...
 constexpr int kGlrBackwardGroups = 768;
 constexpr int kGlrRangeBlocks = 64;   // ... while a range has at most so many blocks
-constexpr int kGlrWholeBlocks = 16;   // the longest sequence that one workgroup walks, in blocks
 
 struct GlrShape {
   int32_t lc_log;

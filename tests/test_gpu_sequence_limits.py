@@ -29,6 +29,34 @@ def test_embedding_of_a_table_past_32_bits():
         assert float(grad.abs().sum(0, dtype=torch.float64)[7]) == 14.0 * k
 
 
+def test_more_tokens_than_one_launch_has_rows_for():
+    """2^27 + 5 tokens of 33 fp16: rows on both sides of the launches' border, and counts as the gradient of ones."""
+    n, rows, dim = 2 ** 27 + 5, 10, 33
+    table = torch.arange(rows * dim, device="cuda").reshape(rows, dim).to(torch.float16)
+    ids = (torch.arange(n, device="cuda") % rows).to(torch.int32)
+    op = SequenceEmbedding(table, padding_id=3)
+    y = op.forward(ids)
+    for t in (0, 2 ** 27 - 1, 2 ** 27, 2 ** 27 + 1, n - 1):
+        assert torch.equal(y[t], table[t % rows] if t % rows != 3 else torch.zeros_like(table[0])), t
+    grad = op.backward(ids, y.fill_(1.0), grad=torch.empty((rows, dim), device="cuda"))
+    want = torch.bincount(ids, minlength=rows).float()          # below 2^24: exact
+    want[3] = 0.0
+    assert torch.equal(grad, want[:, None].expand(rows, dim))
+
+
+def test_more_single_tokens_than_one_launch_has():
+    """2^17 + 2 rows of 65,536 channels; all slots but the first and the last two name no state."""
+    n, dim = 2 ** 17 + 2, dpi.DPI_MAX_DIM
+    x = torch.full((n, dim), 2.0, dtype=torch.float16, device="cuda")
+    gate = torch.zeros((n, dim), dtype=torch.float16, device="cuda")
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    slots[0], slots[n - 2], slots[n - 1] = 1, 0, 2
+    state = torch.tensor([[0.0], [4.0], [8.0]], device="cuda").expand(3, dim).contiguous()
+    y = GatedRecurrence(dim).step(x, gate, state, slots)
+    assert [float(y[b].float().min()) for b in (0, 1, n - 3, n - 2, n - 1)] == [3.0, 0.0, 0.0, 1.0, 5.0]
+    assert state.min(dim=1).values.tolist() == [1.0, 3.0, 5.0] == state.max(dim=1).values.tolist()
+
+
 def test_recurrence_past_32_bits():
     """34 M tokens of 64 fp16 (2.2e9 elements) in three sequences, the last of 700 tokens: as by itself."""
     n, last = 34_000_000, 700
