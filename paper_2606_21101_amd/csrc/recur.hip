@@ -295,6 +295,9 @@ struct Rows {
   __amdgpu_buffer_rsrc_t rsrc;
   int32_t stride, lane;   // bytes; of the thread's first row and channel
   int32_t have;
+  // the non-temporal bit: stores of whole rows past the caches, where nothing of this pass reads them (forward and backward over 441 k tokens of
+  // 128 bf16: 241 -> 232 us)
+  static constexpr int kOnce = 2;
 
   __device__ __forceinline__ Rows(const void* p, int64_t row_stride, const Place& at, const Block& b)
       : stride((int32_t)row_stride * (int32_t)sizeof(T)), have(at.have) {
@@ -333,10 +336,10 @@ struct Rows {
     if constexpr (WIDE) {
       if constexpr (sizeof(T) * V == 16) {
         typedef int quad __attribute__((ext_vector_type(4)));
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(quad, r), rsrc, lane, k * stride, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(quad, r), rsrc, lane, k * stride, kOnce);
       } else {
         typedef int pair __attribute__((ext_vector_type(2)));
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(pair, r), rsrc, lane, k * stride, 0);
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(pair, r), rsrc, lane, k * stride, kOnce);
       }
     } else {
 #pragma unroll
