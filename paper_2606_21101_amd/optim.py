@@ -7,12 +7,17 @@ ask for it, float32 master copies; ``step`` updates them in place on the current
 from __future__ import annotations
 
 import ctypes
+from array import array
+from operator import attrgetter
 from typing import Optional, Sequence
 
 import torch
 
 from . import dpi
 from .sequence import _DT, _here, _on, _refuse
+
+
+_dtype_of = attrgetter("dtype")
 
 
 def _code(dtype: torch.dtype) -> int:
@@ -113,21 +118,30 @@ class AdamW:
             _refuse("one gradient a parameter")
         _here(self.params[0])
         held = self._grad_dtypes
-        dtypes = [d if g is None else g.dtype for g, d in zip(grads, held)]
+        index = torch.cuda.current_device()
+        # one pass of the interpreter's own loops for each property: a call of Python a tensor costs more than the kernel
+        try:
+            addresses = array("Q", map(torch.Tensor.data_ptr, grads))
+            dtypes = list(map(_dtype_of, grads))
+            sound = (list(map(torch.Tensor.numel, grads)) == self._counts and all(map(torch.Tensor.is_contiguous, grads))
+                     and set(map(torch.Tensor.get_device, grads)) == {index})
+        except (AttributeError, TypeError):   # a None among them
+            addresses = array("Q", (0 if g is None else g.data_ptr() for g in grads))
+            dtypes = [d if g is None else g.dtype for g, d in zip(grads, held)]
+            sound = False
+        if not sound:
+            for i, (g, n) in enumerate(zip(grads, self._counts)):
+                if g is not None and (g.numel() != n or g.get_device() != index or not g.is_contiguous()):
+                    _refuse(f"gradient {i} must be contiguous, of the parameter's size, on {self.device}")
         if self._handle is None or dtypes != held:
             self._create(dtypes)
-        index = torch.cuda.current_device()
-        for i, (g, n) in enumerate(zip(grads, self._counts)):
-            if g is not None and (g.numel() != n or g.get_device() != index or not g.is_contiguous()):
-                _refuse(f"gradient {i} must be contiguous, of the parameter's size, on {self.device}")
-        array = self._pointers(*[None if g is None else g.data_ptr() for g in grads])
         t = self.step_count + 1 if step is None else int(step)
         hyper = dpi.dpi_adamw_hyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps,
                                     self.weight_decay, grad_scale, t, self.seed & 0xFFFFFFFF)
         handle, _ = _on(stream)
         if stream is not None:
             self._ws.record_stream(torch.cuda.ExternalStream(handle))
-        dpi.dpi_adamw_step(self._handle, array, hyper, handle)
+        dpi.dpi_adamw_step(self._handle, self._pointers.from_buffer(addresses), hyper, handle)
         self.step_count = t
 
     def _destroy(self) -> None:
