@@ -31,7 +31,7 @@
 // itself runs at 5.5: finding the first sequence takes 5 us, and the workgroups
 // end 27 us apart, as their sequences do); in fp32 152 us forward, 4.5 TB/s.
 // Four histories of 16 to 32 thousand tokens, 64 channels, three launches a
-// pass, 70 us.  Rows that are not whole aligned pieces are read an element at a
+// pass, 65 us.  Rows that are not whole aligned pieces are read an element at a
 // time, which takes 430 us where the first case takes 231, and 49 rather than 31
 // for 4,096 histories of 60 channels of fp32.
 #include "elem.h"
@@ -761,7 +761,8 @@ __global__ __launch_bounds__(kThreads) void glr_maps_kernel(const GlrArgs a) {
 
 // Cut: the ranges' maps to the states that enter them, in place of map_s.  A workgroup takes 4 channels, so that its 256
 // groups of threads walk few ranges each (3,400 ranges of 64 channels: 16 channels and 64 groups took 23 us, most of
-// it waiting for one load after the other); they compose them, join by shuffles and LDS, and walk them again.
+// it waiting for one load after the other; now 857 ranges take 6.7 us); they compose them, join by shuffles and LDS, and
+// walk them again, from registers where they have few (8.9 -> 6.7 us).
 constexpr int kScanThreadsGlr = 1024, kScanChannels = 4, kScanGroups = kScanThreadsGlr / kScanChannels;
 
 template <bool FORWARD>
@@ -773,15 +774,17 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
   const int ch = (int)blockIdx.x * kScanChannels + c;
   const int64_t per = (a.units + kScanGroups - 1) / kScanGroups, begin = min(g * per, a.units), end = min(begin + per, a.units);
   const auto at = [&](int64_t i) { return (FORWARD ? i : a.units - 1 - i) * a.dim + ch; };
-  // eight ranges' maps in flight
-  const auto walk = [&](auto use) {
+  // eight ranges' maps in flight; `held`: there are no more, and they were read before
+  float ma[8], ms[8];
+  const auto walk = [&](bool held, auto use) {
     for (int64_t i0 = begin; i0 < end; i0 += 8) {
-      float ma[8], ms[8];
+      if (!held) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int64_t i = min(i0 + u, end - 1);
-        ma[u] = a.map_a[at(i)];
-        ms[u] = a.map_s[at(i)];
+        for (int u = 0; u < 8; ++u) {
+          const int64_t i = min(i0 + u, end - 1);
+          ma[u] = a.map_a[at(i)];
+          ms[u] = a.map_s[at(i)];
+        }
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
@@ -790,7 +793,7 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
   };
   float A = 1.f, S = 0.f, h = 0.f;
   if (ch < a.dim)
-    walk([&](int64_t, float ma, float ms) {
+    walk(false, [&](int64_t, float ma, float ms) {
       S = mul0(ma, S) + ms;
       A = mul0(ma, A);
     });
@@ -808,11 +811,15 @@ __global__ __launch_bounds__(kScanThreadsGlr) void glr_scan_kernel(const GlrArgs
     ls[wave][c] = S;
   }
   __syncthreads();
-  for (int i = 0; i < wave; ++i) h = mul0(la[i][c], h) + ls[i][c];
+#pragma unroll
+  for (int i = 0; i < kScanWaves - 1; ++i) {
+    const float to = mul0(la[i][c], h) + ls[i][c];
+    h = i < wave ? to : h;
+  }
   const float s0 = __shfl_up(S, kScanChannels, 64), a0 = __shfl_up(A, kScanChannels, 64);
   if (lane >= kScanChannels) h = mul0(a0, h) + s0;
   if (ch < a.dim)
-    walk([&](int64_t i, float ma, float ms) {
+    walk(per <= 8, [&](int64_t i, float ma, float ms) {
       a.map_s[at(i)] = h;
       h = mul0(ma, h) + ms;
     });
