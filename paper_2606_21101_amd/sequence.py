@@ -74,15 +74,21 @@ def _on(stream):
 
 
 class _Workspaces:
-    """Device scratch, one buffer a stream: calls on different streams share none."""
+    """Device scratch, one buffer a stream: calls on different streams share none.  (Every GPU has a stream 0.)
+
+    A call that is captured into a graph takes its own from the graph's memory: one that is held here would be freed
+    when a later call needs more, and the graph's replays would go on writing to it."""
 
     def __init__(self):
         self._held = {}
 
-    def get(self, stream: int, need: int, device) -> torch.Tensor:
-        ws = self._held.get(stream)
+    def get(self, stream: int, need: int, device: torch.device) -> torch.Tensor:
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=device)
+        key = stream, device
+        ws = self._held.get(key)
         if ws is None or ws.numel() < need:
-            ws = self._held[stream] = torch.empty(need, dtype=torch.uint8, device=device)
+            ws = self._held[key] = torch.empty(need, dtype=torch.uint8, device=device)
         return ws
 
 
