@@ -14,6 +14,7 @@ from dataclasses import dataclass
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import dpi
 
@@ -156,6 +157,7 @@ class _EmbedFn(torch.autograd.Function):
         return op.forward(ids)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         (ids,) = ctx.saved_tensors
         if dout.stride(-1) != 1 or dout.stride(0) < dout.shape[1]:
@@ -282,6 +284,7 @@ class _RecurFn(torch.autograd.Function):
         return h, h_last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh, dh_last):
         x, gate, offsets, entry, *rest = ctx.saved_tensors
         if dh is not None and (dh.stride(-1) != 1 or dh.stride(0) < dh.shape[1]):
