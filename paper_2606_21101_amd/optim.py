@@ -32,7 +32,9 @@ class AdamW:
     values with a float32 scale for every 256 elements (m_scale, v_scale), rounded
     at random from `seed`, the step and the element.  m, v, m_scale, v_scale: the
     states to go on from (lists of tensors, updated in place), zeros without.
-    The tensors' memory must stay where it is while the object is used."""
+    The tensors' memory must stay where it is while the object is used, and the
+    object be kept while a graph that holds one of its steps is replayed (such a
+    graph's step number and gradients' addresses are those of its capture)."""
 
     def __init__(self, params: Sequence[torch.Tensor], masters=None, state_bits: int = 32, m=None, v=None,
                  m_scale=None, v_scale=None, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -63,6 +65,9 @@ class AdamW:
         self._pointers = ctypes.c_void_p * len(self.params)
         self._grad_dtypes = [p.dtype for p in self.params]   # until gradients of others come
         self._handle = None
+        self._made = {}   # gradients' dtypes -> handle, its memory, the stream that this was allocated on
+        # autograd counts the changes of what it may have kept for a backward pass
+        self._counted = [p for p in self.params if p.requires_grad]
 
     def _check(self, held, blocks) -> None:
         for i, p in enumerate(self.params):
@@ -90,9 +95,13 @@ class AdamW:
                         _refuse(f"{what}[{i}] must be {blocks[i]} contiguous float32 on {self.device}")
 
     def _create(self, grad_dtypes) -> None:
-        """The library's handle over these tensors (made anew when the gradients' dtypes change)."""
-        torch.cuda.synchronize(self.device)   # a step in flight reads the description that is replaced
-        self._destroy()
+        """The library's handle over these tensors for gradients of these dtypes.  Those for others stay: a captured step
+        may use them."""
+        made = self._made.get(tuple(grad_dtypes))
+        if made is not None:
+            self._handle, self._ws, self._stream = made
+            self._grad_dtypes = grad_dtypes
+            return
         n = len(self.params)
         arr = (dpi.dpi_adamw_tensor * n)()
         for i, p in enumerate(self.params):
@@ -104,8 +113,10 @@ class AdamW:
         if need == 0:
             raise dpi.DpiError(dpi.DPI_ERR_INVALID_ARG, dpi.dpi_last_error())
         self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        torch.cuda.synchronize(self.device)   # ... and its memory may have been another tensor's until now
+        self._stream = _on(None)[0]
+        torch.cuda.synchronize(self.device)   # its memory may have been another tensor's until now
         self._handle = dpi.dpi_adamw_create(arr, self.state_bits, self._ws)
+        self._made[tuple(grad_dtypes)] = self._handle, self._ws, self._stream
         self._grad_dtypes = grad_dtypes
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, step: Optional[int] = None,
@@ -139,16 +150,14 @@ class AdamW:
         hyper = dpi.dpi_adamw_hyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps,
                                     self.weight_decay, grad_scale, t, self.seed & 0xFFFFFFFF)
         handle, _ = _on(stream)
-        if stream is not None:
+        if handle != self._stream:
             self._ws.record_stream(torch.cuda.ExternalStream(handle))
         dpi.dpi_adamw_step(self._handle, self._pointers.from_buffer(addresses), hyper, handle)
         self.step_count = t
-
-    def _destroy(self) -> None:
-        if getattr(self, "_handle", None):
-            dpi.dpi_adamw_destroy(self._handle)
-            self._handle = None
+        if self._counted:
+            torch.autograd.graph.increment_version(self._counted)
 
     def __del__(self):
         if dpi._lib is not None:
-            self._destroy()
+            for handle, _, _ in getattr(self, "_made", {}).values():
+                dpi.dpi_adamw_destroy(handle)

@@ -21,3 +21,30 @@ def test_second_derivatives_are_refused():
     (grad,) = torch.autograd.grad(h.square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         grad.sum().backward()
+
+
+def test_a_step_between_a_graphs_forward_and_backward_is_seen():
+    """Weights that a step changed are not taken for those of the forward pass, as with torch's in-place operations."""
+    w = torch.randn((4, 4), device="cuda", requires_grad=True)
+    x = torch.randn((4, 4), device="cuda", requires_grad=True)
+    y = (x @ w).sum()
+    opt = AdamW([w])
+    opt.step([torch.ones_like(w)])
+    with pytest.raises(RuntimeError):
+        y.backward()
+    (x @ w).sum().backward()
+    # four fp32 terms below 4 in any order: each of three sums rounds by at most 2^-21 of 16
+    assert float((x.grad - w.detach().sum(1)).abs().max()) <= 3 * 16 * 2.0 ** -24 * 2
+
+
+def test_gradients_of_other_dtypes_in_turn():
+    """The states go on from step to step, whatever type each step's gradients have."""
+    torch.manual_seed(0)
+    p = torch.randn(300, device="cuda")
+    q = p.clone()
+    a, b = AdamW([p]), AdamW([q])
+    for k in range(4):
+        g = torch.randn(300, device="cuda").to(torch.bfloat16)
+        a.step([g])
+        b.step([g if k % 2 else g.float()])
+    assert torch.equal(p, q) and torch.equal(a.m[0], b.m[0]) and len(b._made) == 2
