@@ -56,6 +56,12 @@ def _index(t: torch.Tensor, what: str) -> torch.Tensor:
     return t
 
 
+def _status(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    if t is not None and (t.dtype != torch.int32 or t.numel() < 1):
+        _refuse("status must be int32")
+    return t
+
+
 def _states(t: Optional[torch.Tensor], n: int, dim: int, what: str) -> Optional[torch.Tensor]:
     if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (n, dim) or not t.is_contiguous()):
         _refuse(f"{what} must be contiguous float32 {(n, dim)}")
@@ -105,7 +111,7 @@ class SequenceEmbedding:
                  out_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None):
         if table.dim() != 2 or not table.is_contiguous():
             _refuse("table must be a contiguous [num_rows, dim] tensor")
-        self.table, self.scale, self.padding_id, self.status = table, float(scale), int(padding_id), status
+        self.table, self.scale, self.padding_id, self.status = table, float(scale), int(padding_id), _status(status)
         self.num_rows, self.dim = int(table.shape[0]), int(table.shape[1])
         self.out_dtype = out_dtype if out_dtype is not None else table.dtype
         self._code = _dtype(table, "table")
@@ -184,7 +190,7 @@ class GatedRecurrence:
     known); it sets how the work is split, not the result."""
 
     def __init__(self, dim: int, max_len: int = 0, status: Optional[torch.Tensor] = None):
-        self.dim, self.max_len, self.status = int(dim), int(max_len), status
+        self.dim, self.max_len, self.status = int(dim), int(max_len), _status(status)
         self._ws = _Workspaces()
 
     def _desc(self, x, gate, offsets, h0) -> dpi.dpi_glr_desc:

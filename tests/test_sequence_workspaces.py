@@ -1,8 +1,9 @@
-"""The torch classes' device scratch: which calls share a buffer."""
+"""The torch classes' device scratch, which calls share a buffer, and their status words."""
 import pytest
 import torch
 
-from paper_2606_21101_amd.sequence import _Workspaces
+from paper_2606_21101_amd import dpi
+from paper_2606_21101_amd.sequence import GatedRecurrence, SequenceEmbedding, _Workspaces
 
 
 @pytest.fixture
@@ -36,3 +37,11 @@ def test_a_captured_call_shares_none(capturing):
     assert first is not eager and first is not second and first.numel() >= 100
     capturing["is"] = False
     assert ws.get(7, 100, cpu) is eager
+
+
+@pytest.mark.parametrize("status", [torch.zeros(1, dtype=torch.uint8), torch.zeros(1), torch.zeros(0, dtype=torch.int32)])
+def test_a_status_that_is_no_word_is_refused(status):
+    with pytest.raises(dpi.DpiError):
+        SequenceEmbedding(torch.zeros((3, 4)), status=status)
+    with pytest.raises(dpi.DpiError):
+        GatedRecurrence(4, status=status)
