@@ -1,4 +1,4 @@
-"""What autograd is told of the sequence operators and of AdamW."""
+"""What autograd is told of the sequence operators and of AdamW, and that passes leave their inputs as they are."""
 import pytest
 import torch
 
@@ -48,3 +48,33 @@ def test_gradients_of_other_dtypes_in_turn():
         a.step([g])
         b.step([g if k % 2 else g.float()])
     assert torch.equal(p, q) and torch.equal(a.m[0], b.m[0]) and len(b._made) == 2
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dim", [50, 64])
+@pytest.mark.parametrize("max_len", [16, 0])
+def test_passes_leave_their_inputs_and_give_equal_bits(dtype, dim, max_len):
+    """Three training passes that nothing waits between, the second over other histories: the third is as the first."""
+    torch.manual_seed(dim)
+    op = GatedRecurrence(dim, max_len=max_len)
+
+    def inputs(lens):
+        off = torch.zeros(len(lens) + 1, dtype=torch.int32, device="cuda")
+        off[1:] = lens.cumsum(0)
+        n = int(off[-1])
+        x, gate, dh = (torch.randn((n, dim), device="cuda").to(dtype) for _ in range(3))
+        return [x, gate, off, torch.randn((len(lens), dim), device="cuda"), dh, torch.randn((len(lens), dim), device="cuda")]
+
+    def work(x, gate, off, h0, dh, dl):
+        h, last, saved = op.forward(x, gate, off, h0, save=True)
+        return [h, last, *op.backward(saved, dh, dl)]
+
+    lens = torch.randint(0, 17, (3000,), device="cuda")
+    mine, other = inputs(lens), inputs(lens.flip(0))
+    kept = [t.clone() for t in mine]
+    first = work(*mine)
+    work(*other)
+    for a, b in zip(first, work(*mine)):
+        assert torch.equal(a, b)
+    for a, b in zip(mine, kept):
+        assert torch.equal(a, b)
