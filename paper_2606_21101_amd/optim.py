@@ -67,7 +67,7 @@ class AdamW:
         self._handle = None
         self._made = {}   # gradients' dtypes -> handle, its memory, the stream that this was allocated on
         # autograd counts the changes of what it may have kept for a backward pass
-        self._counted = [p for p in self.params if p.requires_grad]
+        self._counted = [p for p in self.params if p.requires_grad and not p.is_inference()]
 
     def _check(self, held, blocks) -> None:
         for i, p in enumerate(self.params):

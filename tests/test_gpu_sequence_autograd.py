@@ -37,6 +37,14 @@ def test_a_step_between_a_graphs_forward_and_backward_is_seen():
     assert float((x.grad - w.detach().sum(1)).abs().max()) <= 3 * 16 * 2.0 ** -24 * 2
 
 
+def test_weights_made_without_autograd_are_stepped():
+    with torch.inference_mode():
+        w = torch.zeros(4, device="cuda", requires_grad=True)
+    AdamW([w], lr=0.5, weight_decay=0.0, eps=0.0).step([torch.ones(4, device="cuda")])
+    # the first step of a constant gradient is lr, but for a few roundings of m, v and their corrections
+    assert float((w.detach() + 0.5).abs().max()) <= 0.5 * 16 * 2.0 ** -24
+
+
 def test_gradients_of_other_dtypes_in_turn():
     """The states go on from step to step, whatever type each step's gradients have."""
     torch.manual_seed(0)
