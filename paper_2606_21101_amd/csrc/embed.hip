@@ -112,14 +112,14 @@ __device__ __forceinline__ void zero_rows(const EmbedGradArgs& a, int share, int
   }
 }
 
-// What the workgroups beside the sort's own do in launch `step` (count, scan, scatter) of a pass: clear the marks in the
-// first launch; the first pass's scatter sets them; every later launch zeroes a share of the rows, with the marks once
-// they are set.  A sort of one pass, of few rows, zeroes them all in the first launch.
+// What the workgroups beside the sort's own do in launch `step` of a pass (count, scan if there is one, scatter): clear the
+// marks in the first launch; the first pass's scatter sets them; every later launch zeroes a share of the rows, with the
+// marks once they are set.  A sort of one pass, of few rows, zeroes them all in the first launch.
 __device__ __forceinline__ void beside_sort(const EmbedGradArgs& a, int pass, int step, int64_t block, int64_t blocks) {
   if (a.passes == 1) {
     if (step == 0) zero_rows<false>(a, 0, block, blocks);
   } else if (pass > 0) {
-    zero_rows<true>(a, 3 * pass + step - 1, block, blocks);
+    zero_rows<true>(a, a.launches * pass + step - 1, block, blocks);
   } else if (step > 0) {
     zero_rows<false>(a, step - 1, block, blocks);
   } else {
@@ -240,13 +240,56 @@ __global__ __launch_bounds__(64 * kSortScanWaves) void sort_scan_kernel(const Em
   if (wave == 0) a.total[b] = all;
 }
 
-template <int ITEMS>
+// The same for a tile by its own workgroup, where the tiles' counts are few (sort_scans): `before`, the counts of the tiles
+// before it, and `total`, of all of them, of the thread's 4 neighbouring digits.  Up to 8 parts of the tiles are read at
+// once, a thread 4 digits of each, and added up in `parts`, 8 words a thread.
+__device__ __forceinline__ void sum_tiles(const EmbedGradArgs& a, int64_t tile, uint32_t* parts, uint32_t* before,
+                                          uint32_t* total) {
+  typedef uint32_t quad __attribute__((ext_vector_type(4)));
+  const int quads = 1 << (a.bits - 2), many = min(kSortThreads / quads, 8);
+  const int q = threadIdx.x & (quads - 1), part = threadIdx.x >> (a.bits - 2);
+  const quad* __restrict__ hist = reinterpret_cast<const quad*>(a.hist);
+  quad low{0, 0, 0, 0}, all{0, 0, 0, 0};
+  if (part < many) {
+    const int tiles = (int)a.tiles, per = (tiles + many - 1) / many, end = min((part + 1) * per, tiles);
+    for (int t0 = part * per; t0 < end; t0 += 16) {
+      quad c[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) c[u] = hist[min(t0 + u, end - 1) * quads + q];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        if (t0 + u >= end) continue;
+        all += c[u];
+        if (t0 + u < tile) low += c[u];
+      }
+    }
+    reinterpret_cast<quad*>(parts)[2 * threadIdx.x] = low;
+    reinterpret_cast<quad*>(parts)[2 * threadIdx.x + 1] = all;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) before[j] = total[j] = 0;
+  if ((int)threadIdx.x < quads) {
+    for (int i = 0; i < many; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        before[j] += parts[(i * quads + threadIdx.x) * 8 + j];
+        total[j] += parts[(i * quads + threadIdx.x) * 8 + 4 + j];
+      }
+    }
+  }
+  __syncthreads();   // `parts` is free again
+}
+
+// SCANNED: a launch before this one made the tiles' prefixes.
+template <int ITEMS, bool SCANNED>
 __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedGradArgs a, int pass) {
   constexpr int kWaves = kSortThreads / 64, kEach = (1 << kSortMaxBits) / kSortThreads;
-  __shared__ uint32_t next[kWaves][1 << kSortMaxBits];
+  static_assert(kEach == 4 && kWaves * (1 << kSortMaxBits) >= 8 * kSortThreads, "what sum_tiles takes");
+  __shared__ __align__(16) uint32_t next[kWaves][1 << kSortMaxBits];
   __shared__ uint32_t sums[kWaves];
   if (blockIdx.x >= a.tiles) {
-    beside_sort(a, pass, 2, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    beside_sort(a, pass, a.launches - 1, blockIdx.x - a.tiles, gridDim.x - a.tiles);
     return;
   }
   const int bins = 1 << a.bits, shift = pass * a.bits;
@@ -262,11 +305,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const EmbedG
   }
   // kEach neighbouring digits a thread: where they start, and this tile's part of them
   uint32_t total[kEach], mine[kEach], sum = 0;
+  if constexpr (!SCANNED) sum_tiles(a, tile, next[0], mine, total);
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     const int b = threadIdx.x * kEach + j;
-    total[j] = b < bins ? a.total[b] : 0;
-    mine[j] = b < bins ? a.hist[(tile << a.bits) + b] : 0;
+    if constexpr (SCANNED) {
+      total[j] = b < bins ? a.total[b] : 0;
+      mine[j] = b < bins ? a.hist[(tile << a.bits) + b] : 0;
+    }
     sum += total[j];
   }
   for (int b = threadIdx.x; b < bins; b += kSortThreads) {
@@ -745,6 +791,14 @@ EmbedGradLayout embed_grad_layout(int64_t num_rows, int32_t dim, int64_t tokens)
   return L;
 }
 
+// Whether the tiles' prefixes take a launch of their own.  Without one each workgroup reads the counts of all tiles, which
+// costs less than a launch while they are few.  Whole gradients of 64 fp16, us, with / without: 5,000 tokens over 200,000
+// rows (2,560 counts) 40 / 35, 20,000 (10,240) 42 / 37, 50,000 (25,088) 43 / 40.5, 110,593 (55,808) 44 / 47.5; 30,000 over
+// 1 M rows (30,720) 55 / 51; 600,000 of 8 over 15 rows (9,376 counts of 586 tiles) 46 / 44.
+static bool sort_scans(const EmbedGradArgs& a) {
+  return a.tiles << a.bits > kSortScanCounts || a.bits < 2 || a.tokens > kSortFewTokens;
+}
+
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t s) {
   if (a.tokens == 0) return hipSuccess;
   if (a.table_dtype == DPI_F32) return forward_by_out<float>(a, s);
@@ -766,20 +820,23 @@ hipError_t launch_embed_grad(const EmbedGradArgs& args, hipStream_t s) {
     e = hipGetLastError();
     if (a.tokens == 0) return e;
   } else {
-    a.zero_shares = a.passes == 1 ? 1 : 3 * a.passes - 1;
+    const bool few = a.tokens <= kSortFewTokens, scans = sort_scans(a);
+    a.launches = scans ? 3 : 2;
+    a.zero_shares = a.passes == 1 ? 1 : a.launches * a.passes - 1;
     const int64_t zero = zero_blocks(a.zero_shares);
     const dim3 tiles((unsigned)(a.tiles + zero)), scan((unsigned)(((1 << a.bits) + 63) / 64 + (zero + 3) / 4));
-    const bool few = a.tokens <= kSortFewTokens;
     for (int p = 0; p < a.passes && e == hipSuccess; ++p) {
       if (few)
         sort_count_kernel<kSortFewItems><<<tiles, kSortThreads, 0, s>>>(a, p);
       else
         sort_count_kernel<kSortManyItems><<<tiles, kSortThreads, 0, s>>>(a, p);
-      sort_scan_kernel<<<scan, 64 * kSortScanWaves, 0, s>>>(a, p);
-      if (few)
-        sort_scatter_kernel<kSortFewItems><<<tiles, kSortThreads, 0, s>>>(a, p);
+      if (scans) sort_scan_kernel<<<scan, 64 * kSortScanWaves, 0, s>>>(a, p);
+      if (!scans)
+        sort_scatter_kernel<kSortFewItems, false><<<tiles, kSortThreads, 0, s>>>(a, p);
+      else if (few)
+        sort_scatter_kernel<kSortFewItems, true><<<tiles, kSortThreads, 0, s>>>(a, p);
       else
-        sort_scatter_kernel<kSortManyItems><<<tiles, kSortThreads, 0, s>>>(a, p);
+        sort_scatter_kernel<kSortManyItems, true><<<tiles, kSortThreads, 0, s>>>(a, p);
       e = hipGetLastError();
     }
   }

@@ -28,6 +28,7 @@ constexpr int kSortThreads = 256;
 constexpr int kSortMaxBits = 10;                            // bits of a digit
 constexpr int kSortFewItems = 4, kSortManyItems = 16;       // items per thread ...
 constexpr int64_t kSortFewTokens = 3 << 18;                 // ... up to this many tokens, beyond
+constexpr int64_t kSortScanCounts = 1 << 15;                // counts of all tiles up to which no launch scans them
 constexpr int kSortOneThreads = 1024, kSortOneItems = 4;    // the workgroup that sorts a short list alone
 constexpr int kSumThreads = 256;
 constexpr int kSumMaxChunk = 32;                            // sorted tokens that one group of lanes sums
@@ -49,6 +50,7 @@ struct EmbedGradArgs {
                        // one that goes on after it
   int32_t passes, bits;
   int64_t tiles;
+  int32_t launches;      // of a pass of the sort
   int32_t zero_shares;   // launches that zero rows
 };
 
